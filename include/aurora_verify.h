@@ -477,6 +477,157 @@ int aurora_draft_loss(const aurora_loss_desc* desc, const float* draft_logits, c
                       const uint16_t* topk_logits, const int8_t* traj, float* row_kl, float* loss_out, float* grad,
                       void* hip_stream);
 
+/*
+ * Block tables and slot maps built on the GPU from request lengths.  After a verification step only the device knows how many of
+ * a request's tokens were kept (section 2.1); this call plans the pages of the next step there, without a trip to the host, and
+ * hands out what aurora_rope_append and aurora_verify_attn take: the lengths, the block table, and for every new token its position
+ * and its slot (page * page_size + offset) in the pools.
+ *
+ * Request b holds held_lens[b] tokens (NULL: none does) and is to hold want_lens[b]:
+ *   fewer   its pages past ceil(want / page_size) go back on top of the stack of free pages (drafts that were rejected, and with 0
+ *           a request that has ended)
+ *   more    pages are taken from the top of the stack for it
+ * All pages given back (requests in order, pages in order) are pushed before the first is taken (in the same order).
+ * A request that wants more is refused, and keeps what it holds, if the stack runs out at it, or the rows do (max_rows); every later
+ * one that wants more is refused too.  So is one whose lengths are negative or longer than its row of the table.
+ *
+ *   block_table [B, max_pages_per_seq]  in: the pages that requests hold; out: the pages taken are written behind them.  Cells
+ *                                       past a request's pages are neither read nor changed (those given back keep their ids).
+ *   free_pages  [num_pages]             the stack; entries 0 .. *free_count - 1 are the free pages, the last one the top
+ *   free_count, free_count_out [1]      how many before, and after; may be the same
+ *   seq_lens    [B]                     the length each request has now; may be held_lens or want_lens
+ *   row_start   [B + 1] or NULL         rows of request b are row_start[b] .. row_start[b + 1] - 1, its new tokens in order
+ *   positions, slots [max_rows]         of every row; from row_start[B] on 0 and -1.  Not used if max_rows is 0: nothing is
+ *                                       then refused for want of rows.
+ *   info        [4] or NULL             rows, pages taken, pages given back, requests refused
+ * The result is unique, hence bit-reproducible.  Given distinct free_count_out and seq_lens the call may be repeated on the
+ * same state with the same result.  Up to 1024 requests and distinct outputs it is one launch, otherwise up to two.
+ * AURORA_ERR_UNSUPPORTED for more than 2^31 - 1 slots or table cells, or rows of the table longer than 2^30 tokens.
+ */
+typedef struct {
+  int32_t batch;             /* B >= 0 (0: the rows and the count are written)                */
+  int32_t page_size;         /* tokens per KV page, >= 1                                      */
+  int32_t max_pages_per_seq; /* row stride of block_table                                     */
+  int64_t num_pages;         /* P, pages in each pool                                         */
+  int32_t max_rows;          /* entries of positions and slots                                */
+} aurora_cache_plan_desc;
+
+int aurora_cache_plan_workspace_bytes(const aurora_cache_plan_desc* desc, size_t* out_bytes);
+int aurora_cache_plan(const aurora_cache_plan_desc* desc, const int32_t* held_lens, const int32_t* want_lens, int32_t* block_table,
+                      int32_t* free_pages, const int32_t* free_count, int32_t* free_count_out, int32_t* seq_lens,
+                      int32_t* row_start, int32_t* positions, int32_t* slots, int32_t* info,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rotary positions, on the way into the paged KV cache that the attention above reads (section 3.1), and back.
+ *
+ *   pair i of a head at position t:  (x, y) -> (x c - y s, y c + x s),  c = magnitude cos(t f_i),  s = magnitude sin(t f_i)
+ *
+ * for the pairs of the first rotary_dim elements of every query and key head - (i, i + rotary_dim / 2), or (2i, 2i + 1) if
+ * interleaved; the other elements pass through.  f_i = frequencies[i] in radians per position, float64 [rotary_dim / 2] on the DEVICE
+ * (aurora_rope_frequencies makes them on the host; a program uploads them once).  Angles are formed and reduced in 64 bits.
+ *
+ *   q [rows, Hq, D], k, v [rows, Hkv, D]   rows may lie apart (the strides): parts of one fused projection's output, say
+ *   positions, slots [rows]                as aurora_cache_plan writes them.  A row with a slot outside 0 .. num_pages * page_size - 1 is
+ *                                          not one (a padded batch): nothing is written for it.  Two rows must not share a slot.
+ *   q_out [rows, Hq, D]                    the turned queries; may be q itself with the same stride
+ *   k_pages, v_pages                       pools [P, Hkv, page_size, D]: turned keys, and values, at their slots
+ * num_kv_heads = 0: queries alone; k, v, k_pages, v_pages are not used and slots may be NULL (every row is one).  num_q_heads = 0: keys
+ * and values alone.  kv_fp8: the pools hold OCP E4M3 codes of value / scale (nearest, ties to even, limited to the largest finite code),
+ * k_scale / v_scale [Hkv] > 0 as in aurora_attn_desc.  Arithmetic in fp32, one rounding at the end.
+ *
+ * aurora_rope_append_backward: from the gradients of q_out and of the pools (float32, as aurora_attn_backward writes them: dq_out with
+ * q_out_stride) to those of q, k and v, of type dtype, rows with q_stride, k_stride and v_stride; zero for rows that are not one.
+ * magnitude included, the turn transposed.  An 8-bit cache is refused (AURORA_ERR_UNSUPPORTED).
+ *
+ * Pointers need the alignment of their element type; whole 16-byte vectors are used where all arrays, strides and rotary_dim allow.
+ * No workspace.  AURORA_ERR_UNSUPPORTED for more than 2^22 rows, head_dim > 256, more than 2^31 - 1 slots.
+ */
+typedef struct {
+  int32_t rows;              /* T >= 0 (0: nothing is enqueued)                               */
+  int32_t num_q_heads;       /* Hq >= 0                                                       */
+  int32_t num_kv_heads;      /* Hkv >= 0, not both 0                                          */
+  int32_t head_dim;          /* D, 1..256                                                     */
+  int32_t rotary_dim;        /* even, 0..D                                                    */
+  int32_t interleaved;       /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1)       */
+  int32_t page_size;
+  int64_t num_pages;         /* P, pages in each pool                                         */
+  int32_t dtype;             /* AURORA_F32 / AURORA_BF16: q, k, v, q_out and (kv_fp8 = 0) the pools */
+  int32_t kv_fp8;
+  const float* k_scale;
+  const float* v_scale;
+  float magnitude;           /* 0 => 1                                                        */
+  int64_t q_stride, k_stride, v_stride, q_out_stride; /* elements from row to row; 0 => contiguous */
+} aurora_rope_desc;
+
+int aurora_rope_append(const aurora_rope_desc* desc, const void* q, const void* k, const void* v, const int32_t* positions,
+                       const int32_t* slots, const double* frequencies, void* q_out, void* k_pages, void* v_pages, void* hip_stream);
+int aurora_rope_append_backward(const aurora_rope_desc* desc, const float* dq_out, const float* dk_pages, const float* dv_pages,
+                                const int32_t* positions, const int32_t* slots, const double* frequencies, void* dq, void* dk, void* dv,
+                                void* hip_stream);
+
+/*
+ * The frequencies of rotary positions, on the HOST: f_i = base^(-2 i / rotary_dim), i < rotary_dim / 2, changed for contexts longer
+ * than the model was trained on.  *magnitude (or NULL) is what goes into aurora_rope_desc with them.  No device is needed.
+ *   AURORA_ROPE_PLAIN    as they are
+ *   AURORA_ROPE_LINEAR   f / factor (position interpolation)
+ *   AURORA_ROPE_BASE     base * factor^(rotary_dim / (rotary_dim - 2)) in place of base (the slowest pair is stretched by factor)
+ *   AURORA_ROPE_BANDS    by the turns that a pair makes over trained_context: f from `high` turns on, f / factor up to `low`, linear in
+ *                        the turns between
+ *   AURORA_ROPE_RAMP     f up to the pair that makes `high` turns, f / factor from the one that makes `low`, linear in the pair's index
+ *                        between (whole indices, rounded outwards); magnitude = 0.1 ln(factor) + 1
+ */
+enum { AURORA_ROPE_PLAIN = 0, AURORA_ROPE_LINEAR = 1, AURORA_ROPE_BASE = 2, AURORA_ROPE_BANDS = 3, AURORA_ROPE_RAMP = 4 };
+typedef struct {
+  int32_t rotary_dim;     /* even, >= 2 (AURORA_ROPE_BASE: >= 4)                              */
+  int32_t kind;
+  double base;            /* > 1                                                              */
+  double factor;          /* >= 1; not used by AURORA_ROPE_PLAIN                              */
+  double trained_context; /* tokens, >= 1; AURORA_ROPE_BANDS and AURORA_ROPE_RAMP             */
+  double low, high;       /* turns, 0 < low < high; the same two                              */
+} aurora_rope_scaling;
+int aurora_rope_frequencies(const aurora_rope_scaling* scaling, double* frequencies, float* magnitude);
+
+/*
+ * Log probabilities of given tokens, entropies and the largest alternatives of rows of logits (appendix A.1, eq. 4) - what a server
+ * returns with the tokens of a step, and what a training step takes the gradient of.  With x = logits / T:
+ *
+ *   lse[m] = log sum_v exp(x_mv)   logprob[m] = x_m,tokens[m] - lse[m]   entropy[m] = lse[m] - sum_v p_mv x_mv,  p_mv = exp(x_mv - lse[m])
+ *   top_ids[m, 0..n_top), top_logprobs: the n_top largest logits of the row, by value descending, equal ones (-0.0 and +0.0 are equal) by
+ *   ascending id, as log probabilities; id -1 / -inf past the end of a row shorter than n_top
+ *
+ * tokens[m] outside 0 .. vocab - 1 (-1, say): the row has no token; logprob 0, no gradient from it.  -inf logits are ordinary smallest
+ * values with probability 0.  A row of nothing else has lse -inf, entropy 0, log probabilities -inf and no gradient.  NaN and +inf make
+ * the row's lse, entropy and log probabilities NaN; its alternatives are then unspecified (valid ids or -1).
+ * tokens and logprob come as a pair; any of logprob, entropy, lse may be NULL, top_ids / top_logprobs iff n_top = 0.
+ *
+ * aurora_token_logprobs_backward: dlogits of type dtype, rows row_stride apart, from dlogprob and dentropy [rows] (either may be NULL: zero)
+ *
+ *   dlogits[m, v] = ( dlogprob[m] ([v = tokens[m]] - p_mv) - dentropy[m] p_mv (log p_mv + entropy[m]) ) / T
+ *
+ * with the entropy (if dentropy is given) and lse that aurora_token_logprobs wrote for the same logits, T and tokens.  dlogits may be logits.
+ * Elements between rows are left as they are.
+ *
+ * Exponentials in fp32, sums over a row in fp64 in a fixed order: bit-reproducible.  The workspace is the forward call's.
+ * AURORA_ERR_UNSUPPORTED for n_top > 32 or more than 2^24 logits a row.
+ */
+typedef struct {
+  int32_t rows;              /* M >= 0 (0: nothing is enqueued)                               */
+  int32_t vocab;             /* V >= 1                                                        */
+  int32_t dtype;             /* AURORA_F32 / AURORA_BF16: type of the logits and their gradient */
+  int32_t n_top;             /* alternatives a row, 0..32                                     */
+  int64_t row_stride;        /* elements from row to row; 0 => vocab                          */
+  float temperature;         /* T; 0 => 1                                                     */
+  const float* temperatures; /* one for every row: DEVICE float32 [rows] (0: 1, as row_lse of a greedy request), or NULL */
+} aurora_logprob_desc;
+
+int aurora_token_logprobs_workspace_bytes(const aurora_logprob_desc* desc, size_t* out_bytes);
+int aurora_token_logprobs(const aurora_logprob_desc* desc, const void* logits, const int32_t* tokens, float* logprob, float* entropy,
+                          float* lse, int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+int aurora_token_logprobs_backward(const aurora_logprob_desc* desc, const void* logits, const int32_t* tokens, const float* entropy,
+                                   const float* lse, const float* dlogprob, const float* dentropy, void* dlogits, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,11 @@ EXPORTS = ("aurora_verify_workspace_bytes", "aurora_verify_attn", "aurora_verify
            "aurora_verify_lmhead", "aurora_verify_accept_logits", "aurora_trace_emit",
            "aurora_verify_logits_ptr", "aurora_status_string", "aurora_verify_check_inputs", "aurora_draft_loss", "aurora_trace_pack", "aurora_attn_backward",
            "aurora_attn_backward_workspace_bytes", "aurora_attn_forward", "aurora_attn_backward_saved", "aurora_debug_set_tree_spin_limit", "aurora_verify_attn_static",
-           "aurora_verify_group_max_ptr", "aurora_probe_contraction")
+           "aurora_verify_group_max_ptr", "aurora_probe_contraction", "aurora_cache_plan", "aurora_cache_plan_workspace_bytes",
+           "aurora_rope_append", "aurora_rope_append_backward", "aurora_rope_frequencies", "aurora_token_logprobs",
+           "aurora_token_logprobs_workspace_bytes", "aurora_token_logprobs_backward")
+
+AURORA_ROPE_PLAIN, AURORA_ROPE_LINEAR, AURORA_ROPE_BASE, AURORA_ROPE_BANDS, AURORA_ROPE_RAMP = range(5)
 
 
 class aurora_attn_desc(C.Structure):
@@ -57,6 +61,29 @@ class aurora_pack_desc(C.Structure):
 class aurora_loss_desc(C.Structure):
     _fields_ = [("rows", C.c_int32), ("draft_vocab", C.c_int32), ("top_k", C.c_int32), ("discard_top_k", C.c_int32),
                 ("lambda_discard", C.c_float)]
+
+
+class aurora_cache_plan_desc(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("page_size", C.c_int32), ("max_pages_per_seq", C.c_int32), ("num_pages", C.c_int64),
+                ("max_rows", C.c_int32)]
+
+
+class aurora_rope_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("page_size", C.c_int32), ("num_pages", C.c_int64),
+                ("dtype", C.c_int32), ("kv_fp8", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("magnitude", C.c_float), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_out_stride", C.c_int64)]
+
+
+class aurora_rope_scaling(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("kind", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("trained_context", C.c_double), ("low", C.c_double), ("high", C.c_double)]
+
+
+class aurora_logprob_desc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("n_top", C.c_int32), ("row_stride", C.c_int64),
+                ("temperature", C.c_float), ("temperatures", C.c_void_p)]
 
 
 class AuroraError(RuntimeError):
@@ -125,6 +152,22 @@ def load():
     lib.aurora_trace_pack.restype = C.c_int
     lib.aurora_draft_loss.argtypes = [C.POINTER(aurora_loss_desc), f32p, i32p, vp, vp, f32p, f32p, f32p, vp]
     lib.aurora_draft_loss.restype = C.c_int
+    lib.aurora_cache_plan_workspace_bytes.argtypes = [C.POINTER(aurora_cache_plan_desc), C.POINTER(C.c_size_t)]
+    lib.aurora_cache_plan_workspace_bytes.restype = C.c_int
+    lib.aurora_cache_plan.argtypes = [C.POINTER(aurora_cache_plan_desc)] + [i32p] * 11 + [vp, C.c_size_t, vp]
+    lib.aurora_cache_plan.restype = C.c_int
+    lib.aurora_rope_append.argtypes = [C.POINTER(aurora_rope_desc)] + [vp] * 10
+    lib.aurora_rope_append.restype = C.c_int
+    lib.aurora_rope_append_backward.argtypes = [C.POINTER(aurora_rope_desc)] + [vp] * 10
+    lib.aurora_rope_append_backward.restype = C.c_int
+    lib.aurora_rope_frequencies.argtypes = [C.POINTER(aurora_rope_scaling), C.POINTER(C.c_double), C.POINTER(C.c_float)]
+    lib.aurora_rope_frequencies.restype = C.c_int
+    lib.aurora_token_logprobs_workspace_bytes.argtypes = [C.POINTER(aurora_logprob_desc), C.POINTER(C.c_size_t)]
+    lib.aurora_token_logprobs_workspace_bytes.restype = C.c_int
+    lib.aurora_token_logprobs.argtypes = [C.POINTER(aurora_logprob_desc), vp, i32p, f32p, f32p, f32p, i32p, f32p, vp, C.c_size_t, vp]
+    lib.aurora_token_logprobs.restype = C.c_int
+    lib.aurora_token_logprobs_backward.argtypes = [C.POINTER(aurora_logprob_desc)] + [vp] * 8
+    lib.aurora_token_logprobs_backward.restype = C.c_int
     lib.aurora_verify_logits_ptr.argtypes = [ad, cd, vp]
     lib.aurora_verify_logits_ptr.restype = C.c_void_p
     lib.aurora_status_string.argtypes = [C.c_int]
@@ -145,6 +188,17 @@ def _ptr(t) -> Optional[int]:
         return t
     if not t.is_contiguous():
         raise ValueError("tensors handed to the library must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
+    """Device address of a tensor whose rows (dimension 0) may lie apart, as the descriptor's stride says."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_contiguous() and t.shape[0] > 1 and (t.stride(0) != stride or not t[0].is_contiguous()):
+        raise ValueError(f"{name}: rows are {t.stride(0)} elements apart, the descriptor says {stride or 'contiguous'}")
+    if t.is_contiguous() and stride and t.shape[0] > 1 and t.stride(0) != stride:
+        raise ValueError(f"{name}: rows are {t.stride(0)} elements apart, the descriptor says {stride}")
     return t.data_ptr()
 
 
@@ -296,6 +350,83 @@ def aurora_draft_loss(desc, draft_logits, topk_ids, topk_logits, traj, row_kl, l
                                   _ptr(row_kl), _ptr(loss_out), _ptr(grad), _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_draft_loss")
+    return st
+
+
+def aurora_cache_plan_workspace_bytes(desc) -> int:
+    out = C.c_size_t(0)
+    st = load().aurora_cache_plan_workspace_bytes(_ref(desc), C.byref(out))
+    if st != AURORA_OK:
+        raise AuroraError(st, "aurora_cache_plan_workspace_bytes")
+    return int(out.value)
+
+
+def aurora_cache_plan(desc, held_lens, want_lens, block_table, free_pages, free_count, free_count_out, seq_lens, row_start,
+                      positions, slots, info, workspace, stream=None, check=True) -> int:
+    wb = workspace.numel() * workspace.element_size()
+    st = load().aurora_cache_plan(_ref(desc), _ptr(held_lens), _ptr(want_lens), _ptr(block_table), _ptr(free_pages),
+                                  _ptr(free_count), _ptr(free_count_out), _ptr(seq_lens), _ptr(row_start), _ptr(positions),
+                                  _ptr(slots), _ptr(info), _ptr(workspace), wb, _stream(stream))
+    if check and st != AURORA_OK:
+        raise AuroraError(st, "aurora_cache_plan")
+    return st
+
+
+def aurora_rope_append(desc, q, k, v, positions, slots, frequencies, q_out, k_pages, v_pages, stream=None, check=True) -> int:
+    """q, k, v and q_out may be tensors whose rows lie apart (views of a fused projection's output): their strides are the descriptor's."""
+    st = load().aurora_rope_append(_ref(desc), _rows_ptr(q, desc.q_stride, "q"), _rows_ptr(k, desc.k_stride, "k"),
+                                   _rows_ptr(v, desc.v_stride, "v"), _ptr(positions), _ptr(slots), _ptr(frequencies),
+                                   _rows_ptr(q_out, desc.q_out_stride, "q_out"), _ptr(k_pages), _ptr(v_pages), _stream(stream))
+    if check and st != AURORA_OK:
+        raise AuroraError(st, "aurora_rope_append")
+    return st
+
+
+def aurora_rope_append_backward(desc, dq_out, dk_pages, dv_pages, positions, slots, frequencies, dq, dk, dv, stream=None,
+                                check=True) -> int:
+    st = load().aurora_rope_append_backward(_ref(desc), _rows_ptr(dq_out, desc.q_out_stride, "dq_out"), _ptr(dk_pages), _ptr(dv_pages),
+                                            _ptr(positions), _ptr(slots), _ptr(frequencies), _rows_ptr(dq, desc.q_stride, "dq"),
+                                            _rows_ptr(dk, desc.k_stride, "dk"), _rows_ptr(dv, desc.v_stride, "dv"), _stream(stream))
+    if check and st != AURORA_OK:
+        raise AuroraError(st, "aurora_rope_append_backward")
+    return st
+
+
+def aurora_rope_frequencies(scaling):
+    """(frequencies, magnitude): a list of rotary_dim / 2 numbers, radians per position, and what multiplies cosine and sine."""
+    f, m = (C.c_double * max(1, scaling.rotary_dim // 2))(), C.c_float(0)
+    st = load().aurora_rope_frequencies(_ref(scaling), f, C.byref(m))
+    if st != AURORA_OK:
+        raise AuroraError(st, "aurora_rope_frequencies")
+    return list(f), m.value
+
+
+def aurora_token_logprobs_workspace_bytes(desc) -> int:
+    out = C.c_size_t(0)
+    st = load().aurora_token_logprobs_workspace_bytes(_ref(desc), C.byref(out))
+    if st != AURORA_OK:
+        raise AuroraError(st, "aurora_token_logprobs_workspace_bytes")
+    return int(out.value)
+
+
+def aurora_token_logprobs(desc, logits, tokens, logprob, entropy, lse, top_ids, top_logprobs, workspace, stream=None,
+                          check=True) -> int:
+    """`logits` may be a tensor (its rows may lie apart) or a raw device address (int), e.g. from aurora_verify_logits_ptr()."""
+    wb = workspace.numel() * workspace.element_size()
+    st = load().aurora_token_logprobs(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"), _ptr(tokens), _ptr(logprob),
+                                      _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), wb,
+                                      _stream(stream))
+    if check and st != AURORA_OK:
+        raise AuroraError(st, "aurora_token_logprobs")
+    return st
+
+
+def aurora_token_logprobs_backward(desc, logits, tokens, entropy, lse, dlogprob, dentropy, dlogits, stream=None, check=True) -> int:
+    st = load().aurora_token_logprobs_backward(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"), _ptr(tokens), _ptr(entropy),
+                                               _ptr(lse), _ptr(dlogprob), _ptr(dentropy),
+                                               _rows_ptr(dlogits, desc.row_stride, "dlogits"), _stream(stream))
+    if check and st != AURORA_OK:
+        raise AuroraError(st, "aurora_token_logprobs_backward")
     return st
 
 

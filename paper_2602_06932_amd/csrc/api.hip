@@ -3,6 +3,9 @@
 #include "common.hpp"
 #include "launch.hpp"
 
+#include <math.h>
+
+#include <initializer_list>
 #include <mutex>
 
 using namespace aurora;
@@ -607,6 +610,257 @@ int aurora_probe_contraction(int mode, const void* operands, size_t operand_byte
     return launch_probe_stream(operands, operand_bytes, (hipStream_t)hip_stream) == hipSuccess ? AURORA_OK : AURORA_ERR_HIP;
   return launch_probe(mode, operands, workgroups, stages, sink, (hipStream_t)hip_stream) == hipSuccess ? AURORA_OK
                                                                                                           : AURORA_ERR_HIP;
+}
+
+namespace {
+bool unaligned(const void* p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+int check_cache_plan(const aurora_cache_plan_desc* d) {
+  if (!d || d->batch < 0 || d->page_size < 1 || d->max_pages_per_seq < 1 || d->num_pages < 1 || d->max_rows < 0)
+    return AURORA_ERR_INVALID_ARG;
+  if ((int64_t)d->max_pages_per_seq * d->page_size > (int64_t)1 << 30) return AURORA_ERR_UNSUPPORTED;
+  if ((int64_t)d->batch * d->max_pages_per_seq > INT32_MAX) return AURORA_ERR_UNSUPPORTED;  // pages are counted in 32 bits,
+  if (d->num_pages > INT32_MAX / d->page_size) return AURORA_ERR_UNSUPPORTED;               // and so are slots
+  return AURORA_OK;
+}
+
+int check_rope(const aurora_rope_desc* d) {
+  if (!d || d->rows < 0 || d->num_q_heads < 0 || d->num_kv_heads < 0 || d->num_q_heads + (int64_t)d->num_kv_heads < 1 ||
+      d->head_dim < 1 || d->rotary_dim < 0 || d->rotary_dim > d->head_dim || d->rotary_dim % 2)
+    return AURORA_ERR_INVALID_ARG;
+  if (d->interleaved != 0 && d->interleaved != 1) return AURORA_ERR_INVALID_ARG;
+  if (d->dtype != AURORA_F32 && d->dtype != AURORA_BF16) return AURORA_ERR_INVALID_ARG;
+  if (d->kv_fp8 != 0 && d->kv_fp8 != 1) return AURORA_ERR_INVALID_ARG;
+  if (!(d->magnitude >= 0.f) || !(d->magnitude < INFINITY)) return AURORA_ERR_INVALID_ARG;
+  if (d->num_kv_heads > 0) {
+    if (d->page_size < 1 || d->num_pages < 1) return AURORA_ERR_INVALID_ARG;
+    if (d->kv_fp8 && (!d->k_scale || !d->v_scale)) return AURORA_ERR_INVALID_ARG;
+    if (d->num_pages > INT32_MAX / d->page_size) return AURORA_ERR_UNSUPPORTED;
+  }
+  const int64_t q = (int64_t)d->num_q_heads * d->head_dim, kv = (int64_t)d->num_kv_heads * d->head_dim;
+  if (d->q_stride < 0 || d->q_out_stride < 0 || d->k_stride < 0 || d->v_stride < 0) return AURORA_ERR_INVALID_ARG;
+  if ((d->q_stride && d->q_stride < q) || (d->q_out_stride && d->q_out_stride < q) || (d->k_stride && d->k_stride < kv) ||
+      (d->v_stride && d->v_stride < kv))
+    return AURORA_ERR_INVALID_ARG;
+  if (d->head_dim > kRopeMaxDim || d->rows > kRopeMaxRows || d->num_q_heads > 65535 || d->num_kv_heads > 65535)
+    return AURORA_ERR_UNSUPPORTED;
+  return AURORA_OK;
+}
+
+RopeLaunch rope_launch_from(const aurora_rope_desc* d) {
+  RopeLaunch a = {};
+  a.rows = d->rows; a.Hq = d->num_q_heads; a.Hkv = d->num_kv_heads; a.D = d->head_dim; a.rotary = d->rotary_dim;
+  a.page = d->num_kv_heads > 0 ? d->page_size : 1;
+  a.num_slots = d->num_kv_heads > 0 ? (int)(d->num_pages * d->page_size) : 0;
+  a.interleaved = d->interleaved != 0; a.bf16 = d->dtype == AURORA_BF16; a.kv_fp8 = d->kv_fp8 != 0 && d->num_kv_heads > 0;
+  a.k_scale = d->k_scale; a.v_scale = d->v_scale;
+  a.magnitude = d->magnitude > 0.f ? d->magnitude : 1.f;
+  const int64_t q = (int64_t)d->num_q_heads * d->head_dim, kv = (int64_t)d->num_kv_heads * d->head_dim;
+  a.q_stride = d->q_stride ? d->q_stride : q; a.q_out_stride = d->q_out_stride ? d->q_out_stride : q;
+  a.k_stride = d->k_stride ? d->k_stride : kv; a.v_stride = d->v_stride ? d->v_stride : kv;
+  return a;
+}
+
+// the arrays that both directions have; rows and the other side's are typed by the caller
+int check_rope_args(const aurora_rope_desc* d, uintptr_t row_type, uintptr_t q_type, uintptr_t pool_type, const void* q, const void* k,
+                    const void* v, const int32_t* positions, const int32_t* slots, const double* frequencies, const void* q_out,
+                    const void* k_pages, const void* v_pages) {
+  if (!positions || (d->rotary_dim > 0 && !frequencies)) return AURORA_ERR_INVALID_ARG;
+  if (d->num_q_heads > 0 && (!q || !q_out)) return AURORA_ERR_INVALID_ARG;
+  if (d->num_kv_heads > 0 && (!k || !v || !slots || !k_pages || !v_pages)) return AURORA_ERR_INVALID_ARG;
+  if (unaligned(positions, 4) || unaligned(slots, 4) || unaligned(frequencies, 8)) return AURORA_ERR_INVALID_ARG;
+  if (d->num_q_heads > 0 && (unaligned(q, row_type) || unaligned(q_out, q_type))) return AURORA_ERR_INVALID_ARG;
+  if (d->num_kv_heads > 0 && (unaligned(k, row_type) || unaligned(v, row_type) || unaligned(k_pages, pool_type) || unaligned(v_pages, pool_type)))
+    return AURORA_ERR_INVALID_ARG;
+  return AURORA_OK;
+}
+
+int run_rope(const aurora_rope_desc* d, bool back, const void* q, const void* k, const void* v, const int32_t* positions, const int32_t* slots,
+             const double* frequencies, void* q_out, void* k_pages, void* v_pages, hipStream_t st) {
+  RopeLaunch a = rope_launch_from(d);
+  if (a.Hq > 0) { a.q = q; a.q_out = q_out; }
+  if (a.Hkv > 0) { a.k = k; a.v = v; a.k_pages = k_pages; a.v_pages = v_pages; }
+  a.positions = positions; a.frequencies = frequencies;
+  a.slots = slots;
+  if (a.Hkv == 0 && slots) a.num_slots = INT32_MAX;  // without a cache a slot only says whether the row is one
+  return launch_rope(a, back, st) == hipSuccess ? AURORA_OK : AURORA_ERR_HIP;
+}
+
+int check_logprob(const aurora_logprob_desc* d) {
+  if (!d || d->rows < 0 || d->vocab < 1 || d->n_top < 0 || d->row_stride < 0 || (d->row_stride && d->row_stride < d->vocab))
+    return AURORA_ERR_INVALID_ARG;
+  if (d->dtype != AURORA_F32 && d->dtype != AURORA_BF16) return AURORA_ERR_INVALID_ARG;
+  if (!(d->temperature >= 0.f) || !(d->temperature < INFINITY)) return AURORA_ERR_INVALID_ARG;
+  if (d->n_top > logprob_max_top() || d->vocab > logprob_max_vocab()) return AURORA_ERR_UNSUPPORTED;
+  return AURORA_OK;
+}
+
+struct LogprobPlan { int splits; size_t keys_off, bytes; };
+LogprobPlan plan_logprob(const aurora_logprob_desc* d) {
+  LogprobPlan p = {};
+  p.splits = logprob_splits(d->rows, d->vocab, d->dtype == AURORA_BF16);
+  const size_t parts = p.splits > 1 ? (size_t)d->rows * p.splits : 0;
+  p.keys_off = align_up(parts * sizeof(LogprobPart));
+  p.bytes = p.keys_off + align_up(parts * d->n_top * sizeof(unsigned long long));
+  if (p.bytes < 256) p.bytes = 256;
+  return p;
+}
+
+LogprobLaunch logprob_launch_from(const aurora_logprob_desc* d) {
+  LogprobLaunch a = {};
+  a.rows = d->rows; a.V = d->vocab; a.n_top = d->n_top; a.bf16 = d->dtype == AURORA_BF16;
+  a.row_stride = d->row_stride ? d->row_stride : d->vocab;
+  a.temperature = d->temperature > 0.f ? d->temperature : 1.f;
+  a.temperatures = d->temperatures;
+  return a;
+}
+}  // namespace
+
+int aurora_cache_plan_workspace_bytes(const aurora_cache_plan_desc* desc, size_t* out_bytes) {
+  if (!out_bytes) return AURORA_ERR_INVALID_ARG;
+  int rc = check_cache_plan(desc);
+  if (rc != AURORA_OK) return rc;
+  *out_bytes = align_up(cache_plan_work_bytes(desc->batch));
+  return AURORA_OK;
+}
+
+int aurora_cache_plan(const aurora_cache_plan_desc* d, const int32_t* held_lens, const int32_t* want_lens, int32_t* block_table,
+                      int32_t* free_pages, const int32_t* free_count, int32_t* free_count_out, int32_t* seq_lens, int32_t* row_start,
+                      int32_t* positions, int32_t* slots, int32_t* info, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_cache_plan(d);
+  if (rc != AURORA_OK) return rc;
+  if (!free_pages || !free_count || !free_count_out) return AURORA_ERR_INVALID_ARG;
+  if (d->batch > 0 && (!want_lens || !block_table || !seq_lens)) return AURORA_ERR_INVALID_ARG;
+  if (d->max_rows > 0 && (!positions || !slots)) return AURORA_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)held_lens, (const void*)want_lens, (const void*)block_table, (const void*)free_pages,
+                        (const void*)free_count, (const void*)free_count_out, (const void*)seq_lens, (const void*)row_start,
+                        (const void*)positions, (const void*)slots, (const void*)info})
+    if (unaligned(p, 4)) return AURORA_ERR_INVALID_ARG;
+  if (!workspace || misaligned(workspace) || workspace_bytes < align_up(cache_plan_work_bytes(d->batch))) return AURORA_ERR_WORKSPACE;
+  if (!have_device()) return AURORA_ERR_HIP;
+  CachePlanLaunch P = {};
+  P.B = d->batch; P.page = d->page_size; P.max_pages = d->max_pages_per_seq; P.num_pages = (int)d->num_pages; P.max_rows = d->max_rows;
+  P.held_lens = held_lens; P.want_lens = want_lens; P.free_count = free_count;
+  P.block_table = block_table; P.free_pages = free_pages; P.free_count_out = free_count_out; P.seq_lens = seq_lens;
+  P.row_start = row_start; P.info = info;
+  if (d->max_rows > 0) { P.positions = positions; P.slots = slots; }
+  P.wide_rows = (((uintptr_t)positions | (uintptr_t)slots) & 15) == 0;
+  P.work = (int32_t*)workspace;
+  return launch_cache_plan(P, (hipStream_t)hip_stream) == hipSuccess ? AURORA_OK : AURORA_ERR_HIP;
+}
+
+int aurora_rope_frequencies(const aurora_rope_scaling* s, double* frequencies, float* magnitude) {
+  if (!s || s->rotary_dim < 2 || s->rotary_dim % 2 || !(s->base > 1.0) || !(s->base < INFINITY)) return AURORA_ERR_INVALID_ARG;
+  const int half = s->rotary_dim / 2;
+  const double two_pi = 6.283185307179586477;
+  if (!frequencies) return AURORA_ERR_INVALID_ARG;
+  const bool scaled = s->kind != AURORA_ROPE_PLAIN;
+  if (scaled && (!(s->factor >= 1.0) || !(s->factor < INFINITY))) return AURORA_ERR_INVALID_ARG;
+  if ((s->kind == AURORA_ROPE_BANDS || s->kind == AURORA_ROPE_RAMP) &&
+      (!(s->trained_context >= 1.0) || !(s->trained_context < INFINITY) || !(s->low > 0.0) || !(s->high > s->low) || !(s->high < INFINITY)))
+    return AURORA_ERR_INVALID_ARG;
+  double base = s->base, lo = 0.0, hi = 0.0;
+  switch (s->kind) {
+    case AURORA_ROPE_PLAIN: case AURORA_ROPE_LINEAR: case AURORA_ROPE_BANDS: break;
+    case AURORA_ROPE_BASE:
+      if (s->rotary_dim < 4) return AURORA_ERR_INVALID_ARG;  // (the exponent has rotary_dim - 2 below the line)
+      base *= pow(s->factor, (double)s->rotary_dim / (s->rotary_dim - 2));
+      break;
+    case AURORA_ROPE_RAMP: {  // the pairs that make `high` and `low` turns over the trained context
+      auto pair_of = [&](double turns) { return s->rotary_dim * log(s->trained_context / (turns * two_pi)) / (2.0 * log(base)); };
+      lo = floor(pair_of(s->high)); hi = ceil(pair_of(s->low));
+      lo = lo < 0.0 ? 0.0 : lo;
+      hi = hi > s->rotary_dim - 1.0 ? s->rotary_dim - 1.0 : hi;
+      if (!(hi > lo)) hi = lo + 0.001;
+      break;
+    }
+    default: return AURORA_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < half; ++i) {
+    const double f = pow(base, -2.0 * i / s->rotary_dim);
+    double keep = 1.0;  // share of the unscaled frequency
+    if (s->kind == AURORA_ROPE_LINEAR) keep = 0.0;
+    if (s->kind == AURORA_ROPE_BANDS) keep = (s->trained_context * f / two_pi - s->low) / (s->high - s->low);
+    if (s->kind == AURORA_ROPE_RAMP) keep = 1.0 - (i - lo) / (hi - lo);
+    keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+    frequencies[i] = keep == 1.0 ? f : keep * f + (1.0 - keep) * f / s->factor;
+  }
+  if (magnitude) *magnitude = s->kind == AURORA_ROPE_RAMP ? (float)(0.1 * log(s->factor) + 1.0) : 1.f;
+  return AURORA_OK;
+}
+
+int aurora_rope_append(const aurora_rope_desc* d, const void* q, const void* k, const void* v, const int32_t* positions,
+                       const int32_t* slots, const double* frequencies, void* q_out, void* k_pages, void* v_pages, void* hip_stream) {
+  int rc = check_rope(d);
+  if (rc != AURORA_OK || d->rows == 0) return rc;
+  const uintptr_t e = d->dtype == AURORA_BF16 ? 2 : 4;
+  rc = check_rope_args(d, e, e, d->kv_fp8 ? 1 : e, q, k, v, positions, slots, frequencies, q_out, k_pages, v_pages);
+  if (rc != AURORA_OK) return rc;
+  if (!have_device()) return AURORA_ERR_HIP;
+  return run_rope(d, false, q, k, v, positions, slots, frequencies, q_out, k_pages, v_pages, (hipStream_t)hip_stream);
+}
+
+int aurora_rope_append_backward(const aurora_rope_desc* d, const float* dq_out, const float* dk_pages, const float* dv_pages,
+                                const int32_t* positions, const int32_t* slots, const double* frequencies, void* dq, void* dk, void* dv,
+                                void* hip_stream) {
+  int rc = check_rope(d);
+  if (rc != AURORA_OK) return rc;
+  if (d->kv_fp8) return AURORA_ERR_UNSUPPORTED;  // an 8-bit cache carries no gradient
+  if (d->rows == 0) return AURORA_OK;
+  const uintptr_t e = d->dtype == AURORA_BF16 ? 2 : 4;
+  rc = check_rope_args(d, e, 4, 4, dq, dk, dv, positions, slots, frequencies, dq_out, dk_pages, dv_pages);
+  if (rc != AURORA_OK) return rc;
+  if (!have_device()) return AURORA_ERR_HIP;
+  return run_rope(d, true, dq, dk, dv, positions, slots, frequencies, (void*)dq_out, (void*)dk_pages, (void*)dv_pages, (hipStream_t)hip_stream);
+}
+
+int aurora_token_logprobs_workspace_bytes(const aurora_logprob_desc* desc, size_t* out_bytes) {
+  if (!out_bytes) return AURORA_ERR_INVALID_ARG;
+  int rc = check_logprob(desc);
+  if (rc != AURORA_OK) return rc;
+  *out_bytes = plan_logprob(desc).bytes;
+  return AURORA_OK;
+}
+
+int aurora_token_logprobs(const aurora_logprob_desc* d, const void* logits, const int32_t* tokens, float* logprob, float* entropy,
+                          float* lse, int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_logprob(d);
+  if (rc != AURORA_OK || d->rows == 0) return rc;
+  if (!logits || (tokens != nullptr) != (logprob != nullptr)) return AURORA_ERR_INVALID_ARG;
+  if (d->n_top > 0 && (!top_ids || !top_logprobs)) return AURORA_ERR_INVALID_ARG;
+  if (!logprob && !entropy && !lse && d->n_top == 0) return AURORA_ERR_INVALID_ARG;  // nothing requested
+  if (unaligned(logits, d->dtype == AURORA_BF16 ? 2 : 4)) return AURORA_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)tokens, (const void*)logprob, (const void*)entropy, (const void*)lse, (const void*)top_ids,
+                        (const void*)top_logprobs, (const void*)d->temperatures})
+    if (unaligned(p, 4)) return AURORA_ERR_INVALID_ARG;
+  const LogprobPlan plan = plan_logprob(d);
+  if (!workspace || misaligned(workspace) || workspace_bytes < plan.bytes) return AURORA_ERR_WORKSPACE;
+  if (!have_device()) return AURORA_ERR_HIP;
+  LogprobLaunch a = logprob_launch_from(d);
+  a.logits = logits; a.tokens = tokens; a.logprob = logprob; a.entropy = entropy; a.lse = lse;
+  a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  a.splits = plan.splits;
+  a.parts = (LogprobPart*)workspace;
+  a.keys = (unsigned long long*)((char*)workspace + plan.keys_off);
+  return launch_logprob(a, (hipStream_t)hip_stream) == hipSuccess ? AURORA_OK : AURORA_ERR_HIP;
+}
+
+int aurora_token_logprobs_backward(const aurora_logprob_desc* d, const void* logits, const int32_t* tokens, const float* entropy,
+                                   const float* lse, const float* dlogprob, const float* dentropy, void* dlogits, void* hip_stream) {
+  int rc = check_logprob(d);
+  if (rc != AURORA_OK || d->rows == 0) return rc;
+  if (!logits || !lse || !dlogits || (!dlogprob && !dentropy)) return AURORA_ERR_INVALID_ARG;
+  if ((dlogprob && !tokens) || (dentropy && !entropy)) return AURORA_ERR_INVALID_ARG;
+  const uintptr_t e = d->dtype == AURORA_BF16 ? 2 : 4;
+  if (unaligned(logits, e) || unaligned(dlogits, e)) return AURORA_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)tokens, (const void*)entropy, (const void*)lse, (const void*)dlogprob, (const void*)dentropy,
+                        (const void*)d->temperatures})
+    if (unaligned(p, 4)) return AURORA_ERR_INVALID_ARG;
+  if (!have_device()) return AURORA_ERR_HIP;
+  LogprobLaunch a = logprob_launch_from(d);
+  a.logits = logits; a.tokens = tokens; a.entropy = (float*)entropy; a.lse = (float*)lse; a.dlogprob = dlogprob; a.dentropy = dentropy;
+  a.grad = dlogits;
+  return launch_logprob_backward(a, (hipStream_t)hip_stream) == hipSuccess ? AURORA_OK : AURORA_ERR_HIP;
 }
 
 const char* aurora_status_string(int status) {

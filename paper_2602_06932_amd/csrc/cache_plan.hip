@@ -1,0 +1,274 @@
+// Block tables and slot maps of the paged KV cache, built on the GPU from request lengths.  After a verification step (paper
+// section 2.1: a prefix of the drafts is kept) only the GPU knows how long each request has become; this plans the pages of
+// the next one without a trip to the host.
+//
+//   pages(n) = ceil(n / page).  A request that holds h tokens and is to hold w gives pages(h) - pages(w) back if w < h, and takes
+//   pages(w) - pages(h) if w > h.  All pages given back go on top of the stack of free pages, in order; then pages are taken from the
+//   top, in order.  With F given back onto n free ones, the k-th page taken is therefore the (F - 1 - k)-th given back if k < F, and
+//   stack entry n - 1 - (k - F) if not - and of the pages given back the first F - taken are all that reaches the stack.
+//
+// So the state after the call is a function of three prefix sums over the requests (pages given back, pages taken, token rows), and
+// no order between writes is needed: cells of the table that are read (pages held, pages given back) are never written, stack
+// entries that are read lie below those that are written.  Tokens of a page taken in this call find it the same way, not through
+// the table.
+//
+// Bound by latency, except where it writes a position and a slot for each of a million rows.  Up to 1024 requests every workgroup forms
+// the prefix sums itself, four requests a thread, and does its share of the writing: one launch.  Where more than one workgroup
+// is wanted and an output is the input that the others still read, or there are more requests, one workgroup plans into the workspace
+// and a second launch writes.
+#include "launch.hpp"
+
+#include <algorithm>
+
+namespace aurora {
+
+constexpr int kPlanThreads = 256;
+constexpr int kPlanPer = 4;                              // requests a thread
+constexpr int kPlanChunk = kPlanThreads * kPlanPer;      // requests planned at a time
+constexpr int kPlanWaves = kPlanThreads / kWave;
+
+// What the writing needs: per request the first row, page taken and page given back, the tokens held, and the table column at which
+// the pages taken or given back start; then the stack's size and the totals.
+struct PlanArrays { int32_t *row, *take, *give, *held, *col; };
+struct PlanTotals { int n, freed, taken, rows; };
+
+struct PlanReq { int held, want, col, need, back; int64_t rows; bool grow, shrink, differs; };
+
+__device__ __forceinline__ int pages_of(int tokens, int page) { return (int)(((unsigned)tokens + (unsigned)page - 1u) / (unsigned)page); }
+
+__device__ __forceinline__ PlanReq plan_request(const CachePlanLaunch& P, int b) {
+  PlanReq r = {};
+  if (b >= P.B) return r;
+  r.held = P.held_lens ? P.held_lens[b] : 0;
+  r.want = P.want_lens[b];
+  r.differs = r.want != r.held;
+  if (r.held < 0 || r.want < 0) return r;
+  const int hp = pages_of(r.held, P.page), wp = pages_of(r.want, P.page);
+  if (hp > P.max_pages || wp > P.max_pages) return r;
+  r.grow = r.want > r.held;
+  r.shrink = r.want < r.held;
+  r.col = min(hp, wp);
+  r.need = r.grow ? wp - hp : 0;
+  r.back = r.shrink ? hp - wp : 0;
+  r.rows = r.grow ? (int64_t)r.want - r.held : 0;
+  return r;
+}
+
+struct PlanSums { int back, need; int64_t rows; };
+
+// exclusive prefix of the threads' sums over the workgroup, and the totals
+__device__ __forceinline__ PlanSums plan_scan(const PlanSums& mine, PlanSums& total, PlanSums* s_wave) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  PlanSums x = mine;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int b = __shfl_up(x.back, o, kWave), n = __shfl_up(x.need, o, kWave);
+    const long long r = __shfl_up((long long)x.rows, o, kWave);
+    if (lane >= o) { x.back += b; x.need += n; x.rows += r; }
+  }
+  __syncthreads();  // (the last chunk's sums may still be read)
+  if (lane == 63) s_wave[wave] = x;
+  __syncthreads();
+  total = {0, 0, 0};
+  PlanSums before = {0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const PlanSums t = s_wave[w];
+    if (w < wave) { before.back += t.back; before.need += t.need; before.rows += t.rows; }
+    total.back += t.back; total.need += t.need; total.rows += t.rows;
+  }
+  return {before.back + x.back - mine.back, before.need + x.need - mine.need, before.rows + x.rows - mine.rows};
+}
+
+// The plan of all requests, by one workgroup; A may lie in LDS (one chunk) or in the workspace.  publish: this workgroup writes
+// the results that are not shared out.
+template <bool kOneChunk>
+__device__ __forceinline__ PlanTotals plan_requests(const CachePlanLaunch& P, const PlanArrays& A, bool publish) {
+  __shared__ PlanSums s_wave[kPlanWaves];
+  __shared__ int s_cut, s_refused;
+  __shared__ int s_cut_need;
+  __shared__ int64_t s_cut_rows;
+  const int tid = threadIdx.x;
+  const int n = min(max(P.free_count[0], 0), P.num_pages);
+  if (tid == 0) { s_cut = INT32_MAX; s_refused = 0; }
+
+  int freed = 0;
+  if constexpr (!kOneChunk) {  // the pages given back, before anyone is granted a page
+    PlanSums all = {0, 0, 0};
+    for (int b0 = tid; b0 < P.B; b0 += kPlanThreads) all.back += plan_request(P, b0).back;
+    PlanSums t;
+    plan_scan(all, t, s_wave);
+    freed = t.back;
+  }
+  PlanSums carry = {0, 0, 0};
+  for (int base = 0; kOneChunk ? base == 0 : base < P.B; base += kPlanChunk) {
+    PlanReq r[kPlanPer];
+    PlanSums mine = {0, 0, 0}, total;
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i) {
+      r[i] = plan_request(P, base + tid * kPlanPer + i);
+      mine.back += r[i].back; mine.need += r[i].need; mine.rows += r[i].rows;
+    }
+    PlanSums at = plan_scan(mine, total, s_wave);
+    if constexpr (kOneChunk) freed = total.back;
+    at.back += carry.back; at.need += carry.need; at.rows += carry.rows;
+    carry.back += total.back; carry.need += total.need; carry.rows += total.rows;
+    // The sums never fall, so those who are refused for want of pages or rows are one run of growing requests up to the last: the
+    // first of them is all there is to find.
+    PlanSums cum = at;
+    int refused = 0, first = INT32_MAX;
+    PlanSums at_first = {0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i) {
+      const bool fits = (int64_t)cum.need + r[i].need <= (int64_t)n + freed && (!P.slots || cum.rows + r[i].rows <= P.max_rows);
+      const bool short_of = r[i].grow && !fits;
+      if (short_of && first == INT32_MAX) { first = base + tid * kPlanPer + i; at_first = cum; }
+      refused += short_of || (r[i].differs && !r[i].grow && !r[i].shrink);
+      cum.need += r[i].need; cum.rows += r[i].rows;
+    }
+    if (first != INT32_MAX) atomicMin(&s_cut, first);
+    if (refused) atomicAdd(&s_refused, refused);
+    __syncthreads();
+    if (first != INT32_MAX && s_cut == first) { s_cut_need = at_first.need; s_cut_rows = at_first.rows; }
+    __syncthreads();
+    const int cut = s_cut;
+    cum = at;
+#pragma unroll
+    for (int i = 0; i < kPlanPer; ++i) {
+      const int b = base + tid * kPlanPer + i;
+      if (b < P.B) {
+        const bool past = b >= cut;
+        const int row = (int)(past ? s_cut_rows : cum.rows), take = past ? s_cut_need : cum.need;
+        A.row[b] = row; A.take[b] = take; A.give[b] = cum.back; A.held[b] = r[i].held; A.col[b] = r[i].col;
+        if (publish) {
+          P.seq_lens[b] = r[i].shrink || (r[i].grow && !past) ? r[i].want : r[i].held;
+          if (P.row_start) P.row_start[b] = row;
+        }
+      }
+      cum.back += r[i].back; cum.need += r[i].need; cum.rows += r[i].rows;
+    }
+  }
+  if constexpr (!kOneChunk) __syncthreads();
+  PlanTotals t;
+  const bool cut = s_cut != INT32_MAX;
+  t.n = n;
+  t.freed = freed;
+  t.taken = cut ? s_cut_need : carry.need;
+  t.rows = (int)(cut ? s_cut_rows : carry.rows);
+  if (tid == 0) { A.row[P.B] = t.rows; A.take[P.B] = t.taken; A.give[P.B] = t.freed; }
+  if (publish && tid == 0) {
+    if (P.row_start) P.row_start[P.B] = t.rows;
+    P.free_count_out[0] = (int)min((int64_t)n + freed - t.taken, (int64_t)P.num_pages);
+    if (P.info) { P.info[0] = t.rows; P.info[1] = t.taken; P.info[2] = t.freed; P.info[3] = s_refused; }
+  }
+  return t;
+}
+
+// the request whose run of `start` holds x: the last b with start[b] <= x (start[0] = 0, x < start[B])
+__device__ __forceinline__ int plan_owner(const int32_t* start, int B, int x) {
+  int lo = 0, hi = B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (start[mid] <= x) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ int given_page(const CachePlanLaunch& P, const PlanArrays& A, int j) {
+  const int b = plan_owner(A.give, P.B, j);
+  return P.block_table[(size_t)b * P.max_pages + A.col[b] + (j - A.give[b])];
+}
+__device__ __forceinline__ int taken_page(const CachePlanLaunch& P, const PlanArrays& A, const PlanTotals& t, int k) {
+  return k < t.freed ? given_page(P, A, t.freed - 1 - k) : P.free_pages[t.n - 1 - (k - t.freed)];
+}
+
+// the table cells, stack entries and rows of this workgroup
+__device__ __forceinline__ void plan_write(const CachePlanLaunch& P, const PlanArrays& A, const PlanTotals& t) {
+  const int first = blockIdx.x * kPlanThreads + threadIdx.x, step = gridDim.x * kPlanThreads;
+  for (int k = first; k < t.taken; k += step) {
+    const int b = plan_owner(A.take, P.B, k);
+    P.block_table[(size_t)b * P.max_pages + A.col[b] + (k - A.take[b])] = taken_page(P, A, t, k);
+  }
+  for (int j = first; j < t.freed - t.taken; j += step)
+    if ((int64_t)t.n + j < P.num_pages) P.free_pages[t.n + j] = given_page(P, A, j);
+  if (!P.slots) return;
+  // four rows a thread: one search, one page for all of them more often than not
+  for (int64_t r0 = (int64_t)first * 4; r0 < P.max_rows; r0 += (int64_t)step * 4) {
+    int pos[4], slot[4];
+    int b = 0, left = 0, at = 0, pg = 0, off = 0, pid = 0;  // left: rows of request b from here on
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = (int)r0 + e;
+      if (r >= t.rows) { pos[e] = 0; slot[e] = -1; continue; }
+      const bool enter = left == 0;
+      if (enter) {
+        b = plan_owner(A.row, P.B, r);
+        left = A.row[b + 1] - r;
+        at = A.held[b] + (r - A.row[b]);
+        pg = at / P.page;
+        off = at - pg * P.page;
+      } else if (off == P.page) {
+        ++pg;
+        off = 0;
+      }
+      if (enter || off == 0) {
+        const int col = A.col[b];
+        pid = pg < col ? P.block_table[(size_t)b * P.max_pages + pg] : taken_page(P, A, t, A.take[b] + pg - col);
+      }
+      pos[e] = at++;
+      slot[e] = (int)((unsigned)pid * (unsigned)P.page + (unsigned)off++);
+      --left;
+    }
+    if (P.wide_rows && r0 + 4 <= P.max_rows) {
+      *(int4*)(P.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *(int4*)(P.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (r0 + e < P.max_rows) { P.positions[r0 + e] = pos[e]; P.slots[r0 + e] = slot[e]; }
+    }
+  }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanLaunch P) {
+  __shared__ int32_t s_row[kPlanChunk + 1], s_take[kPlanChunk + 1], s_give[kPlanChunk + 1], s_held[kPlanChunk], s_col[kPlanChunk];
+  const PlanArrays A = {s_row, s_take, s_give, s_held, s_col};
+  const PlanTotals t = plan_requests<true>(P, A, blockIdx.x == 0);
+  __syncthreads();
+  plan_write(P, A, t);
+}
+
+__device__ __forceinline__ PlanArrays workspace_arrays(const CachePlanLaunch& P) {
+  const size_t n = (size_t)P.B + 1;
+  int32_t* w = P.work + 4;
+  return {w, w + n, w + 2 * n, w + 3 * n, w + 4 * n};
+}
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_requests_kernel(CachePlanLaunch P) {
+  const PlanTotals t = plan_requests<false>(P, workspace_arrays(P), true);
+  if (threadIdx.x == 0) *(int4*)P.work = make_int4(t.n, t.freed, t.taken, t.rows);
+}
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_write_kernel(CachePlanLaunch P) {
+  const int4 t = *(const int4*)P.work;
+  plan_write(P, workspace_arrays(P), PlanTotals{t.x, t.y, t.z, t.w});
+}
+
+size_t cache_plan_work_bytes(int batch) { return 16 + 5 * ((size_t)batch + 1) * sizeof(int32_t); }
+
+hipError_t launch_cache_plan(const CachePlanLaunch& P, hipStream_t st) {
+  // A workgroup per 1024 rows or 4096 cells of the table, whichever asks for more (how many cells change hands only the lengths say).
+  const int64_t rows = P.slots ? ((int64_t)P.max_rows + 1023) / 1024 : 0;
+  const int64_t cells = ((int64_t)P.B * P.max_pages + 4095) / 4096;
+  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(rows, cells), 1024));
+  // an output that replaces an input is safe within one workgroup alone: the others read the input too
+  const bool in_place = P.free_count_out == P.free_count || P.seq_lens == P.held_lens || P.seq_lens == P.want_lens;
+  if (P.B <= kPlanChunk && (grid == 1 || !in_place)) {
+    hipLaunchKernelGGL(cache_plan_kernel, dim3(grid), dim3(kPlanThreads), 0, st, P);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(cache_plan_requests_kernel, dim3(1), dim3(kPlanThreads), 0, st, P);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(cache_plan_write_kernel, dim3(grid), dim3(kPlanThreads), 0, st, P);
+  return hipGetLastError();
+}
+
+}  // namespace aurora

@@ -159,4 +159,57 @@ struct CheckLaunch {
 };
 hipError_t launch_check_inputs(const CheckLaunch& c, hipStream_t st);
 
+// block tables and slot maps from request lengths (see cache_plan.hip)
+struct CachePlanLaunch {
+  int B, page, max_pages, num_pages, max_rows;
+  bool wide_rows;                                          // positions and slots start at 16 bytes
+  const int32_t *held_lens, *want_lens, *free_count;       // held_lens may be NULL
+  int32_t *block_table, *free_pages, *free_count_out, *seq_lens;
+  int32_t *row_start, *positions, *slots, *info;           // or NULL (positions and slots together)
+  int32_t* work;                                           // cache_plan_work_bytes(B)
+};
+size_t cache_plan_work_bytes(int batch);
+hipError_t launch_cache_plan(const CachePlanLaunch& P, hipStream_t st);
+
+// rotary positions into the paged cache and back (see rope.hip)
+struct RopeLaunch {
+  int rows, Hq, Hkv, D, rotary, page, num_slots;
+  bool interleaved, bf16, kv_fp8;
+  const float *k_scale, *v_scale;
+  float magnitude;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;      // elements from row to row
+  const int32_t *positions, *slots;                        // slots: NULL where there is no cache
+  const double* frequencies;
+  // in: rows of q, k and v, and where they go.  Back: q, k and v are the gradients' rows, written; q_out and the pools are read, fp32
+  const void *q, *k, *v;
+  void *q_out, *k_pages, *v_pages;
+  int block_rows;                                          // set by the launcher
+};
+constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;   // what the launch's second dimension and a block's angles in LDS allow
+hipError_t launch_rope(const RopeLaunch& P, bool back, hipStream_t st);
+
+// log probabilities of given tokens, entropy, alternatives, and the gradient (see logprob.hip)
+struct LogprobPart { double s, t; float r, pad; };
+struct LogprobLaunch {
+  int rows, V, n_top;
+  bool bf16, wide;
+  int64_t row_stride;
+  float temperature;
+  const float* temperatures;                               // [rows] or NULL
+  const void* logits;
+  const int32_t* tokens;
+  float *logprob, *entropy, *lse, *top_logprobs;
+  int32_t* top_ids;
+  const float *dlogprob, *dentropy;
+  void* grad;
+  int splits;                                              // workgroups a row
+  LogprobPart* parts;                                      // [rows, splits], and their n_top sorted keys each, where splits > 1
+  unsigned long long* keys;
+};
+int logprob_splits(int64_t rows, int V, bool bf16);
+int logprob_max_top();
+int logprob_max_vocab();
+hipError_t launch_logprob(const LogprobLaunch& P, hipStream_t st);
+hipError_t launch_logprob_backward(const LogprobLaunch& P, hipStream_t st);
+
 }  // namespace aurora
