@@ -189,7 +189,7 @@ constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;   // what the launch's 
 hipError_t launch_rope(const RopeLaunch& P, bool back, hipStream_t st);
 
 // log probabilities of given tokens, entropy, alternatives, and the gradient (see logprob.hip)
-struct LogprobPart { double s, t; float r, pad; };
+struct LogprobPart { double s, t; float m, pad; };
 struct LogprobLaunch {
   int rows, V, n_top;
   bool bf16, wide;

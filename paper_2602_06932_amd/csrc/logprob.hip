@@ -4,10 +4,11 @@
 //   lse = log sum_v e^x_v     logprob = x_t - lse     H = lse - sum_v p_v x_v     p_v = e^(x_v - lse)
 //   dz_v = [ g_l (delta_vt - p_v) - g_H p_v (log p_v + H) ] / T
 //
-// Forward: bound by the one read of the logits.  A thread keeps a running reference r, s = sum e^(x - r) and t = sum (x - r) e^(x - r)
-// in units of log 2, so that H = log s - t / s takes no second pass; moving the reference by d turns (s, t) into (s, t + d s) 2^d.
-// Sixteen or 32 elements are summed in 32 bits at a time, their sums in 64: a row may have a million entries.  r is the value that was
-// really subtracted, rounded as it is, and the outputs are formed from it, so that its rounding cancels.
+// Forward: bound by the one read of the logits.  A thread keeps the largest logit m so far, the reference r of it, s = sum e^(x - r) and
+// t = sum (x - r) e^(x - r), in units of log 2, so that H = log s - t / s takes no second pass; moving the reference by d turns (s, t)
+// into (s, t + d s) 2^d.  Sixteen or 32 elements are summed in 32 bits at a time, their sums in 64: a row may have a million
+// entries.  r is the value that was really subtracted, rounded as it is, and the outputs are formed from it, so that its rounding
+// cancels.  Logits so large that x leaves fp32's range (a mask of the type's lowest value, and nothing else left) are subtracted first.
 // A row goes to one workgroup where there are many; few rows are split, and a second launch joins the parts.
 //
 // Alternatives ride in the same pass at three lane exchanges and one LDS write per 128 (16-bit: 256) elements: the maximum of every such
@@ -86,35 +87,41 @@ __device__ __forceinline__ LpPart lp_part(const T* row, int V, int split, int sp
   return p;
 }
 
-struct LpSums { float r; double s, t; };
-__device__ __forceinline__ LpSums lp_join(const LpSums& a, const LpSums& b) {
-  const float r = fmaxf(a.r, b.r), ref = r == -INFINITY ? 0.f : r;
-  const double da = a.r == -INFINITY ? 0.0 : (double)a.r - ref, db = b.r == -INFINITY ? 0.0 : (double)b.r - ref;
-  const double fa = (double)__builtin_amdgcn_exp2f((float)da), fb = (double)__builtin_amdgcn_exp2f((float)db);
-  // (one that is far below counts for nothing, and its distance must not turn 0 into NaN)
-  const double ta = fa > 0 ? fa * (a.t + da * a.s) : 0.0, tb = fb > 0 ? fb * (b.t + db * b.s) : 0.0;
-  return {r, fa * a.s + fb * b.s, ta + tb};
+// what is subtracted for the reference m: its rounded multiple, or, past kLpFar / c, m itself before the product
+constexpr float kLpFar = 8.5e37f;
+__device__ __forceinline__ bool lp_far(float m, float c) { return fabsf(m) * c > kLpFar; }
+__device__ __forceinline__ double lp_ref(float m, float c) { return lp_far(m, c) ? (double)m * (double)c : (double)(m * c); }
+
+struct LpSums { float m; double s, t; };
+// the sums with reference `to` (the largest of several, c as above); nothing so far counts for nothing
+__device__ __forceinline__ LpSums lp_moved(const LpSums& a, float to, float c) {
+  if (a.m == to) return a;
+  if (a.m == -INFINITY) return {to, a.s, a.t};  // (zeros, or NaN)
+  const float d = (float)(lp_ref(a.m, c) - lp_ref(to, c));
+  const double f = (double)__builtin_amdgcn_exp2f(d);
+  // (far below: its distance must not turn 0 into NaN)
+  return {to, f * a.s, f > 0 ? f * (a.t + (double)d * a.s) : 0.0 * a.s};
 }
 
 // the row's numbers from its sums (a row without anything finite has lse -inf and entropy 0); returns the logsumexp in units of log 2
 __device__ __forceinline__ double lp_finish(const LogprobLaunch& P, size_t row, const LpSums& x, float c, float z_t, bool known) {
-  const bool none = x.s == 0.0 && x.r == -INFINITY;
-  const double l2 = none ? 0.0 : log2(x.s);
-  if (P.lse) P.lse[row] = none ? -INFINITY : (float)(kLpLn2 * ((double)x.r + l2));
+  const bool none = x.s == 0.0 && x.m == -INFINITY;
+  const double l2 = none ? 0.0 : log2(x.s), r = lp_ref(x.m, c);
+  if (P.lse) P.lse[row] = none ? -INFINITY : (float)(kLpLn2 * (r + l2));
   if (P.entropy) P.entropy[row] = none ? 0.f : (float)(kLpLn2 * (l2 - x.t / x.s));
   if (P.logprob) {
     float lp = 0.f;
-    if (known) lp = none || z_t == -INFINITY ? -INFINITY : (float)(kLpLn2 * ((double)z_t * (double)c - (double)x.r - l2));
+    if (known) lp = none || z_t == -INFINITY ? -INFINITY : (float)(kLpLn2 * ((double)z_t * (double)c - r - l2));
     P.logprob[row] = lp;
   }
-  return (double)x.r + l2;
+  return r + l2;
 }
 
-__device__ __forceinline__ float lp_scale(const LogprobLaunch& P, size_t row) {  // log2(e) / T
-  float T = P.temperatures ? P.temperatures[row] : P.temperature;
-  if (!(T > 0.f)) T = 1.f;
-  return kLpLog2e / T;
+__device__ __forceinline__ float lp_temperature(const LogprobLaunch& P, size_t row) {
+  const float T = P.temperatures ? P.temperatures[row] : P.temperature;
+  return T > 0.f ? T : 1.f;
 }
+__device__ __forceinline__ float lp_scale(const LogprobLaunch& P, size_t row) { return kLpLog2e / lp_temperature(P, row); }
 
 // ---- selection of the n largest of a workgroup's part -------------------------------------------------------------------
 struct LpLds {
@@ -330,19 +337,21 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
   const float z_t = known ? to_f32<T>(z[token]) : 0.f;
 
   LpSums mine = {-INFINITY, 0.0, 0.0};
+  float neg = 0.f;  // minus the reference
+  bool far = false;
   // takes elements into the running sums (top: their maximum)
-  auto add = [&](const auto& x, float top) {
+  auto add = [&](auto& x, float top) {
     constexpr int n = (int)(sizeof(x) / sizeof(float));
-    const float peak = top * c;
-    if (peak > mine.r) {
-      const float d = mine.r == -INFINITY ? 0.f : mine.r - peak;
-      const double f = (double)__builtin_amdgcn_exp2f(d);
-      mine.t = f * (mine.t + (double)d * mine.s);
-      mine.s *= f;
-      if (!(f > 0)) mine.t = 0.0;
-      mine.r = peak;
+    if (top > mine.m) {
+      mine = lp_moved(mine, top, c);
+      neg = -(mine.m * c);
+      far = lp_far(mine.m, c);
     }
-    const float neg = mine.r == -INFINITY ? 0.f : -mine.r;
+    if (far) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) x[i] -= mine.m;
+      neg = 0.f;
+    }
     float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < n; ++i) {
@@ -387,13 +396,15 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
   {  // the elements outside whole vectors: one each for the first threads
     const int before = w.first - w.lo, edges = before + w.hi - w.tail;
     float x[1] = {-INFINITY};
+    float top = -INFINITY;
     if (tid < edges) {
       x[0] = to_f32<T>(z[tid < before ? w.lo + tid : w.tail + tid - before]);
-      add(x, x[0]);
+      top = fmaxf(x[0], -INFINITY);  // (not a NaN)
+      add(x, top);
     }
     if constexpr (kTop) {
       if (wave == 0) {
-        const float top = wave_max(x[0]);
+        top = wave_max(top);
         if (lane == 0) s_lds.bm[kLpBlocks] = top;
       }
     }
@@ -401,21 +412,25 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
 
   // ---- the workgroup's sums ------------------------------------------------------------------------------------
   {
-    const float r = wave_max(mine.r), ref = r == -INFINITY ? 0.f : r;
-    const float d = mine.r == -INFINITY ? 0.f : mine.r - ref;
-    const double f = (double)__builtin_amdgcn_exp2f(d);
-    double t = f > 0 ? f * (mine.t + (double)d * mine.s) : 0.0, s = f * mine.s;
-    s = wave_sum(s);
-    t = wave_sum(t);
-    if (lane == 0) s_part[wave] = {r, s, t};
+    const float m = wave_max(mine.m);
+    mine = lp_moved(mine, m, c);
+    const double s = wave_sum(mine.s), t = wave_sum(mine.t);
+    if (lane == 0) s_part[wave] = {m, s, t};
   }
   __syncthreads();
   if (tid == 0) {
-    LpSums all = s_part[0];
+    float m = s_part[0].m;
 #pragma unroll
-    for (int i = 1; i < kLpWaves; ++i) all = lp_join(all, s_part[i]);
+    for (int i = 1; i < kLpWaves; ++i) m = fmaxf(m, s_part[i].m);
+    LpSums all = {m, 0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < kLpWaves; ++i) {
+      const LpSums x = lp_moved(s_part[i], m, c);
+      all.s += x.s;
+      all.t += x.t;
+    }
     if (P.splits == 1) s_lse2 = lp_finish(P, row, all, c, z_t, known);
-    else P.parts[task] = LogprobPart{all.s, all.t, all.r, 0.f};
+    else P.parts[task] = LogprobPart{all.s, all.t, all.m, 0.f};
   }
   if constexpr (kTop) {
     if (P.splits > 1) {
@@ -453,12 +468,11 @@ __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobL
     LpSums x = {-INFINITY, 0.0, 0.0};
     if (tid < parts) {
       const LogprobPart p = P.parts[row * parts + tid];
-      x = {p.r, p.s, p.t};
+      x = {p.m, p.s, p.t};
     }
-    const float r = wave_max(x.r), ref = r == -INFINITY ? 0.f : r;
-    const float d = x.r == -INFINITY ? 0.f : x.r - ref;
-    const double f = (double)__builtin_amdgcn_exp2f(d);
-    const double t = wave_sum(f > 0 ? f * (x.t + (double)d * x.s) : 0.0), s = wave_sum(f * x.s);
+    const float m = wave_max(x.m);
+    x = lp_moved(x, m, c);
+    const double s = wave_sum(x.s), t = wave_sum(x.t);
     if (n > 0) {
       const unsigned long long head = tid < parts ? P.keys[(row * parts + tid) * n] : 0ull;
       int above = 0;
@@ -470,7 +484,7 @@ __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobL
       const int token = P.tokens ? P.tokens[row] : -1;
       const bool known = token >= 0 && token < P.V;
       const float z_t = known ? to_f32<T>(((const T*)P.logits)[row * (size_t)P.row_stride + token]) : 0.f;
-      s_lse2 = lp_finish(P, row, {r, s, t}, c, z_t, known);
+      s_lse2 = lp_finish(P, row, {m, s, t}, c, z_t, known);
     }
   }
   if (n == 0) return;
@@ -514,20 +528,18 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
   const LpPart w = lp_part(z, P.V, split, P.splits);
   const u32x4_t* vp = (const u32x4_t*)(z + w.first);
 
-  const float c = lp_scale(P, row), inv_t = c * (float)kLpLn2;
+  const float inv_t = 1.f / lp_temperature(P, row);
   const float lse = P.lse[row];
   const bool any = !(lse == -INFINITY);
   const int token = P.tokens ? P.tokens[row] : -1;
   const float gl = any && P.dlogprob && token >= 0 && token < P.V ? P.dlogprob[row] * inv_t : 0.f;
   const float gh = any && P.dentropy ? P.dentropy[row] * inv_t : 0.f;
-  // dz = p (a + b log2 p) + [v = t] gl
-  const float a = -fmaf(gh, P.dentropy ? P.entropy[row] : 0.f, gl), b = -gh * (float)kLpLn2;
-  const float neg = any ? -lse * kLpLog2e : 0.f;
-  auto one = [&](float x, int id) {
-    const float d = fmaf(x, c, neg);
-    const float e = __builtin_amdgcn_exp2f(d);
-    const float v = e * fmaf(b, fmaxf(d, kLpFloor), a);
-    return id == token ? v + gl : v;
+  // dz = p (a - g_H log p) + [v = t] g_l, log p held between the floor and 0 (a row's NaN is in a)
+  const float a = lse != lse ? lse : -fmaf(gh, P.dentropy ? P.entropy[row] : 0.f, gl);
+  const float neg = any ? -lse : 0.f;
+  auto one = [&](float x) {
+    const float l = __builtin_amdgcn_fmed3f(fmaf(x, inv_t, neg), kLpFloor, 0.f);
+    return __builtin_amdgcn_exp2f(l * kLpLog2e) * fmaf(-gh, l, a);
   };
 
   for (int v0 = 0; v0 < w.vecs; v0 += kLpBackThreads * kLpBackVecs) {
@@ -541,15 +553,17 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
       float x[kV];
       lp_widen<T>(raw[u], x);
       const int id = w.first + vec * kV;
+#pragma unroll
+      for (int e = 0; e < kV; ++e) x[e] = one(x[e]);
+      if ((unsigned)(token - id) < (unsigned)kV) {  // one vector of the row (g_l is 0 where there is no token)
+#pragma unroll
+        for (int e = 0; e < kV; ++e) x[e] += id + e == token ? gl : 0.f;
+      }
       u32x4_t o;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-          o[i] = __float_as_uint(one(x[i], id + i));
-        } else {
-          const f32x2_t pr = {one(x[2 * i], id + 2 * i), one(x[2 * i + 1], id + 2 * i + 1)};
-          o[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(pr, bf16x2_t));
-        }
+        if constexpr (sizeof(T) == 4) o[i] = __float_as_uint(x[i]);
+        else o[i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{x[2 * i], x[2 * i + 1]}), bf16x2_t));
       }
       if (P.wide) {
         *(u32x4_t*)(g + id) = o;
@@ -569,7 +583,7 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
   const int before = w.first - w.lo, edges = before + w.hi - w.tail;
   if (tid < edges) {
     const int id = tid < before ? w.lo + tid : w.tail + tid - before;
-    g[id] = from_f32<T>(one(to_f32<T>(z[id]), id));
+    g[id] = from_f32<T>(one(to_f32<T>(z[id])) + (id == token ? gl : 0.f));
   }
 }
 

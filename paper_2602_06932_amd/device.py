@@ -169,6 +169,27 @@ class DeviceVerify:
             raise B.AuroraError(st, "aurora_trace_emit")
         return st
 
+    def logprobs(self, tokens, n_top=0, after="verify", stream=None):
+        """Log probabilities of `tokens` (int32 device tensor [B, Nq], -1 where there is none; the step's next_token or y_out, say),
+        entropies and the n_top largest alternatives at the step's temperature, from the logits that the last verify / accept call left."""
+        w = self.w
+        rows = w.batch * w.num_q
+        if getattr(self, "_logprob_k", None) != (n_top, after):
+            # one temperature per token row: requests' own where they have them (a greedy request's rows at temperature 1)
+            self._row_temps = None if self.temperatures is None else self.temperatures.repeat_interleave(w.num_q)
+            self.logprob_desc = B.aurora_logprob_desc(
+                rows=rows, vocab=w.vocab, dtype=B.AURORA_F32, n_top=n_top, temperature=w.temperature,
+                temperatures=None if self._row_temps is None else self._row_temps.data_ptr())
+            self.logprob, self.entropy, self.lse = (torch.empty((w.batch, w.num_q), dtype=torch.float32, device="cuda") for _ in range(3))
+            self.top_ids = torch.empty((rows, n_top), dtype=torch.int32, device="cuda") if n_top else None
+            self.top_logprobs = torch.empty((rows, n_top), dtype=torch.float32, device="cuda") if n_top else None
+            self._logprob_ws = torch.empty(B.aurora_token_logprobs_workspace_bytes(self.logprob_desc), dtype=torch.uint8, device="cuda")
+            self._logprob_logits = B.aurora_verify_logits_ptr(self.attn_desc if after == "verify" else None, self.accept_desc,
+                                                              self.workspace)
+            self._logprob_k = (n_top, after)
+        return B.aurora_token_logprobs(self.logprob_desc, self._logprob_logits, tokens, self.logprob, self.entropy, self.lse,
+                                       self.top_ids, self.top_logprobs, self._logprob_ws, stream)
+
     def attn_via_binding(self, stream=None):
         return B.aurora_verify_attn(self.attn_desc, self.q, self.k_pages, self.v_pages, self.block_table,
                                     self.seq_lens, self.parents, self.attn_out, self.workspace, stream)

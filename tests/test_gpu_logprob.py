@@ -1,0 +1,264 @@
+"""Token log probabilities, entropies, alternatives and the gradient against the float64 oracle.
+
+Tolerances, per row, with x = z / T, m = max x, p the probabilities and u = 2^-24 (half a step of fp32):
+  log2(e) / T is rounded twice: all x are off by the same factor 1 +- 2u;
+  an exponent d = (x - m) log2 e is one fused product, off by u |d|, its exponential by 2u more, the sums of at most 32 values by 10 u:
+  a weight p is off by e = u (2 |x - m| + 16), relative.
+  lse      2u max|x| + sum p e + u |lse|          (the common factor moves lse by at most max |x| times itself)
+  logprob  2u |x_t - E x| + sum p e + u |logprob|
+  entropy  2u Var x + sum p e (|log p + H| + 1) + 16 u sum p |x - m| + u H
+  dz       p off by u (2 |x| + 2 |lse| + 2 |log p| + 16): the logsumexp is handed over in fp32; log p + H by u (2 |x| + 2 |lse| + 2 H + 8);
+           half a step of the result on top (bfloat16: 2^-8)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle.operators_oracle import token_logprobs, token_logprobs_backward
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+
+
+def _logits(seed, M, V, dtype, kind="normal"):
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn(M, V, generator=g) * 2.5
+    if kind == "peaked":
+        z[torch.arange(M), torch.randint(0, V, (M,), generator=g)] += 15
+    if kind == "masked":          # minus infinity, the lowest finite value, a row with nothing left, rows with less than the alternatives
+        z[:, torch.rand(V, generator=g) < 0.3] = -float("inf")
+        z[:, torch.rand(V, generator=g) < 0.1] = torch.finfo(DT[dtype]).min
+        z[0] = -float("inf")
+        if M > 2:
+            z[1, 2:] = -float("inf")
+            z[1, :2] = 1.0
+            z[2] = torch.finfo(DT[dtype]).min
+    if kind == "equal":
+        z[:] = 0.25
+        z[M // 2:] = torch.randint(0, 2, (M - M // 2, V), generator=g).float()
+        z[0] = torch.where(torch.arange(V) % 2 == 0, 0.0, -0.0)
+    if kind == "rising":          # the largest ones side by side
+        z = torch.linspace(-8, 8, V).expand(M, V).clone()
+        z[M // 2:] = z[M // 2:].flip(1)
+    return z.to(DT[dtype])
+
+
+def _place(z, stride, shift):
+    """z on the GPU with rows `stride` apart, starting `shift` elements past an aligned address; and the whole buffer."""
+    M, V = z.shape
+    buf = torch.full((shift + M * stride + 8,), 3.0, dtype=z.dtype, device="cuda")
+    view = torch.as_strided(buf, (M, V), (stride, 1), shift)
+    view.copy_(z)
+    return view, buf
+
+
+def _run(av, z, tokens, T, n_top, stride=0, shift=0, temps=None):
+    M, V = z.shape
+    view, buf = _place(z, stride or V, shift)
+    d = av.aurora_logprob_desc(rows=M, vocab=V, dtype=av.AURORA_F32 if z.dtype == torch.float32 else av.AURORA_BF16, n_top=n_top,
+                               row_stride=stride, temperature=T, temperatures=None if temps is None else temps.data_ptr())
+    nan = lambda *s: torch.full(s, float("nan"), device="cuda")
+    o = dict(logprob=nan(M), entropy=nan(M), lse=nan(M), top_ids=torch.full((M, n_top), -7, dtype=torch.int32, device="cuda") if n_top else None,
+             top_logprobs=nan(M, n_top) if n_top else None)
+    ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    tok = torch.from_numpy(np.asarray(tokens, np.int32)).cuda()
+    av.aurora_token_logprobs(d, view, tok, o["logprob"], o["entropy"], o["lse"], o["top_ids"], o["top_logprobs"], ws)
+    torch.cuda.synchronize()
+    return {k: None if v is None else v.cpu().numpy() for k, v in o.items()}, (d, view, buf, tok, o)
+
+
+def _inf_close(got, ref, tol):
+    same = np.isneginf(ref)
+    assert np.array_equal(np.isneginf(got), same)
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got - ref)
+    assert np.isfinite(got[~same]).all() and (off[~same] <= tol[~same]).all(), (off[~same] - tol[~same]).max()
+
+
+def _check(av, z, tokens, T=1.0, n_top=0, temps=None, grad=True, seed=0, **kw):
+    M, V = z.shape
+    print(f"[case] {M} x {V} {z.dtype} n_top={n_top} T={T} {kw}", flush=True)
+    got, (d, view, buf, tok, o) = _run(av, z, tokens, T, n_top, temps=temps, **kw)
+    Tr = np.full(M, T) if temps is None else np.where(temps.cpu().numpy() > 0, temps.cpu().numpy(), 1.0)
+    zz = z.double().numpy()
+    ref = token_logprobs(zz, tokens, Tr, n_top)
+    x = zz / Tr[:, None]
+    fin = np.where(np.isfinite(x), x, 0.0)
+    lse0 = np.where(np.isneginf(ref["lse"]), 0.0, ref["lse"])
+    lp = np.where(np.isfinite(x), x - lse0[:, None], 0.0)
+    p = np.where(np.isfinite(x), np.exp(x - lse0[:, None]), 0.0)
+    dist = np.where(p > 0, np.abs(fin - np.where(p > 0, fin, -np.inf).max(1, initial=-np.inf, keepdims=True)), 0.0)
+    e = U * (2 * dist + 16)
+    pe = (p * e).sum(1)
+    mean = (p * fin).sum(1)
+    top = np.where(p > 0, np.abs(fin), 0.0).max(1)     # (values without weight do not move the sums)
+    x_t = fin[np.arange(M), np.clip(tokens, 0, V - 1)]
+    _inf_close(got["lse"], ref["lse"], 2 * U * top + pe + U * np.abs(lse0))
+    _inf_close(got["logprob"], ref["logprob"], 2 * U * np.abs(x_t - mean) + pe + U * np.where(np.isfinite(ref["logprob"]), np.abs(ref["logprob"]), 0))
+    H = ref["entropy"]
+    var = (p * (fin - mean[:, None]) ** 2).sum(1)
+    tol_h = 2 * U * var + (p * e * (np.abs(lp + H[:, None]) + 1)).sum(1) + 16 * U * (p * dist).sum(1) + U * H
+    _inf_close(got["entropy"], H, tol_h)
+    if n_top:
+        assert np.array_equal(got["top_ids"], ref["top_ids"])
+        picked = np.take_along_axis(fin, np.clip(ref["top_ids"], 0, None), 1)
+        tl = np.where(np.isfinite(ref["top_logprobs"]), np.abs(ref["top_logprobs"]), 0)
+        _inf_close(got["top_logprobs"], ref["top_logprobs"], 2 * U * np.abs(picked - mean[:, None]) + pe[:, None] + U * tl)
+    if not grad:
+        return
+    rng = np.random.default_rng(seed)
+    gl, gh = rng.standard_normal((2, M)).astype(np.float32)
+    gref = token_logprobs_backward(zz, tokens, Tr, gl.astype(np.float64), gh.astype(np.float64))
+    tolp = U * (2 * np.abs(fin) + 2 * np.abs(lse0)[:, None] + 2 * np.abs(lp) + 16)
+    tol = p * (np.abs(gl)[:, None] * tolp + np.abs(gh)[:, None] * (np.abs(lp + H[:, None]) * tolp + U * (2 * np.abs(fin) + 2 * np.abs(lse0)[:, None] + 2 * H[:, None] + 8) + tol_h[:, None]))
+    tol = tol / Tr[:, None] + 4 * U * np.abs(gl)[:, None] / Tr[:, None] + (2.0 ** -8 if z.dtype == torch.bfloat16 else 4 * U) * np.abs(gref) + 1e-38
+    dl, de = torch.from_numpy(gl).cuda(), torch.from_numpy(gh).cuda()
+    before = buf.clone()
+    # where the logits' rows lie, and elsewhere within 16 bytes
+    for out in (torch.full_like(buf, 9.0), torch.full((buf.numel() + 1,), 9.0, dtype=buf.dtype, device="cuda")[1:]):
+        gview = torch.as_strided(out, view.shape, view.stride(), view.storage_offset() + out.storage_offset())
+        av.aurora_token_logprobs_backward(d, view, tok, o["entropy"], o["lse"], dl, de, gview)
+        torch.cuda.synchronize()
+        g = gview.double().cpu().numpy()
+        assert np.isfinite(g).all() and (np.abs(g - gref) <= tol).all(), (np.abs(g - gref) - tol).max()
+        rest = torch.ones_like(out, dtype=torch.bool)
+        torch.as_strided(rest, view.shape, view.stride(), view.storage_offset()).fill_(False)
+        assert (out[rest] == 9.0).all()                    # between the rows, and around them
+    assert torch.equal(buf.view(torch.uint8), before.view(torch.uint8))
+    av.aurora_token_logprobs_backward(d, view, tok, o["entropy"], o["lse"], dl, de, view)  # in place
+    torch.cuda.synchronize()
+    assert torch.equal(view, torch.as_strided(out, view.shape, view.stride(), view.storage_offset() + out.storage_offset()))
+
+
+def _tokens(seed, M, V):
+    t = np.random.default_rng(seed).integers(0, V, M)
+    if M > 3:
+        t[1], t[3] = -1, V
+    return t
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 31, 100, 777, 2049, 16001, 32003])
+def test_vocabularies_short_and_odd(gpu_lib, vocab, dtype):
+    for M, n_top, T in ((1, 5, 1.0), (6, 32, 0.7), (6, 1, 1.5)):
+        _check(gpu_lib, _logits(vocab + M, M, vocab, dtype), _tokens(vocab, M, vocab), T, n_top)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["peaked", "masked", "equal", "rising"])
+def test_rows_that_are_masked_equal_or_sorted(gpu_lib, kind, dtype):
+    for M, V, n_top in ((6, 50, 8), (6, 5003, 32), (7, 70001, 20)):
+        _check(gpu_lib, _logits(V, M, V, dtype, kind), _tokens(V, M, V), 1.0, n_top, grad=V < 60000)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_full_vocabularies_and_many_rows(gpu_lib, dtype):
+    _check(gpu_lib, _logits(1, 5, 128256, dtype, "peaked"), _tokens(1, 5, 128256), 1.0, 5)
+    _check(gpu_lib, _logits(2, 40, 128257, dtype), _tokens(2, 40, 128257), 0.7, 20, grad=False)
+    _check(gpu_lib, _logits(3, 700, 4099, dtype), _tokens(3, 700, 4099), 1.0, 3)
+
+
+@pytest.mark.parametrize("kind", ["masked", "equal", "rising"])
+def test_one_workgroup_a_row(gpu_lib, kind):
+    """So many rows that none is split: the selection's rare paths write the results themselves."""
+    for dtype in ("f32", "bf16"):
+        z = _logits(5, 520, 9001, dtype, kind)
+        _check(gpu_lib, z, _tokens(5, 520, 9001), 1.0, 32, grad=False)
+
+
+def test_rows_longer_than_a_workgroup_takes(gpu_lib):
+    _check(gpu_lib, _logits(6, 520, 300001, "f32")[:520], _tokens(6, 520, 300001), 1.0, 4, grad=False)
+    z = _logits(7, 1, 1 << 24, "bf16")
+    _check(gpu_lib, z, [12345678], 1.0, 32, grad=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_rows_apart_and_not_aligned(gpu_lib, shift, dtype):
+    for V, stride in ((1000, 1024), (1003, 1111), (5, 9)):
+        _check(gpu_lib, _logits(V, 9, V, dtype), _tokens(V, 9, V), 0.9, 6, stride=stride, shift=shift)
+
+
+def test_a_temperature_for_every_row(gpu_lib):
+    temps = torch.tensor([0.5, 0.0, 1.0, 2.0, 0.0, 0.1, 3.0], device="cuda")
+    _check(gpu_lib, _logits(9, 7, 3001, "f32"), _tokens(9, 7, 3001), 1.0, 7, temps=temps)
+
+
+def test_nan_and_infinity_reach_the_results_of_their_row_alone(gpu_lib):
+    z = _logits(10, 6, 5000, "f32")
+    z[1, 77], z[2, 4999], z[4] = float("nan"), float("inf"), float("nan")
+    tok = np.full(6, 5)
+    got, (d, view, buf, t, o) = _run(gpu_lib, z, tok, 1.0, 8)
+    ref = token_logprobs(z[[0, 3, 5]].double().numpy(), tok[[0, 3, 5]], 1.0, 8)
+    for k in ("lse", "entropy", "logprob"):
+        assert np.isnan(got[k][[1, 2, 4]]).all(), k
+        assert np.allclose(got[k][[0, 3, 5]], ref[k], rtol=1e-5, atol=1e-6)
+    assert np.array_equal(got["top_ids"][[0, 3, 5]], ref["top_ids"])
+    assert ((got["top_ids"] >= -1) & (got["top_ids"] < 5000)).all()
+    g = torch.zeros_like(view)
+    ones = torch.ones(6, device="cuda")
+    gpu_lib.aurora_token_logprobs_backward(d, view, t, o["entropy"], o["lse"], ones, ones, g)
+    torch.cuda.synchronize()
+    assert torch.isnan(g[[1, 2, 4]]).any(1).all() and torch.isfinite(g[[0, 3, 5]]).all()
+
+
+def test_parts_of_the_results_and_either_gradient(gpu_lib):
+    av = gpu_lib
+    z = _logits(11, 4, 3000, "f32").cuda()
+    tok = torch.tensor([5, -1, 2999, 0], dtype=torch.int32, device="cuda")
+    d = av.aurora_logprob_desc(rows=4, vocab=3000, dtype=av.AURORA_F32)
+    ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    e = lambda: torch.zeros(4, device="cuda")
+    lp, H, lse, H2, lse2 = e(), e(), e(), e(), e()
+    av.aurora_token_logprobs(d, z, tok, lp, H, lse, None, None, ws)
+    av.aurora_token_logprobs(d, z, None, None, None, lse2, None, None, ws)
+    av.aurora_token_logprobs(d, z, None, None, H2, None, None, None, ws)
+    assert torch.equal(lse, lse2) and torch.equal(H, H2)
+    gl, gh = torch.randn(4, device="cuda"), torch.randn(4, device="cuda")
+    a, b, both = (torch.zeros_like(z) for _ in range(3))
+    av.aurora_token_logprobs_backward(d, z, tok, None, lse, gl, None, a)
+    av.aurora_token_logprobs_backward(d, z, None, H, lse, None, gh, b)
+    av.aurora_token_logprobs_backward(d, z, tok, H, lse, gl, gh, both)
+    torch.cuda.synchronize()
+    ref = token_logprobs_backward(z.double().cpu().numpy(), tok.cpu().numpy(), 1.0, gl.double().cpu().numpy(), None)
+    assert np.allclose(a.cpu().numpy(), ref, rtol=1e-5, atol=1e-7)
+    assert torch.allclose(a + b, both, rtol=1e-5, atol=1e-7)
+
+
+def test_two_graphs_and_a_stream_of_its_own(gpu_lib):
+    """Captured calls on new logits; the workspace's contents do not matter from one call to the next."""
+    av = gpu_lib
+    M, V, n = 12, 40000, 6
+    z = _logits(12, M, V, "f32").cuda()
+    tok = torch.arange(M, dtype=torch.int32, device="cuda") * 3
+    d = av.aurora_logprob_desc(rows=M, vocab=V, dtype=av.AURORA_F32, n_top=n)
+    ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    new = lambda: [torch.zeros(M, device="cuda") for _ in range(3)] + [torch.zeros((M, n), dtype=torch.int32, device="cuda"), torch.zeros((M, n), device="cuda")]
+    a, b, ref = new(), new(), new()
+    g = torch.zeros_like(z)
+    torch.cuda.synchronize()
+
+    def step(o):
+        av.aurora_token_logprobs(d, z, tok, *o, ws)
+        av.aurora_token_logprobs_backward(d, z, tok, o[1], o[2], o[0], o[1], g)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(a)
+    side.synchronize()
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1):
+        step(a)
+    with torch.cuda.graph(g2):
+        step(b)
+    for k in range(3):
+        z.copy_(torch.randn_like(z) * 3)
+        ws.fill_(0xff)
+        g1.replay()
+        g2.replay()
+        torch.cuda.synchronize()
+        gg = g.clone()
+        step(ref)
+        torch.cuda.synchronize()
+        for x, y, r in zip(a, b, ref):
+            assert torch.equal(x, r) and torch.equal(y, r)
+        assert torch.equal(gg, g)

@@ -1,0 +1,191 @@
+"""A run of the operators together, as a server and a trainer use them: lengths -> pages and slots -> rotary positions into the cache ->
+attention over it -> LM head and acceptance -> log probabilities -> lengths again; and the gradient back through attention and
+rotation.  References are dense and in float64."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import gen
+from oracle.operators_oracle import cache_plan, rope_turn, token_logprobs
+
+pytestmark = pytest.mark.gpu
+
+
+class Server:
+    """Pools, block table, free pages and lengths on the GPU; the host keeps only what it needs to check."""
+
+    def __init__(self, av, B, hq, hkv, d, page, width, dtype):
+        self.av, self.B, self.hq, self.hkv, self.d, self.page, self.width = av, B, hq, hkv, d, page, width
+        self.dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.code = av.AURORA_BF16 if dtype == "bf16" else av.AURORA_F32
+        self.P = B * width + 3
+        self.kp, self.vp = (torch.full((self.P, hkv, page, d), float("nan"), dtype=self.dt, device="cuda") for _ in range(2))
+        self.table = torch.full((B, width), -1, dtype=torch.int32, device="cuda")
+        self.free = torch.randperm(self.P, device="cuda").to(torch.int32)
+        self.count = torch.tensor([self.P], dtype=torch.int32, device="cuda")
+        self.lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+        self.freqs = torch.tensor(av.aurora_rope_frequencies(av.aurora_rope_scaling(rotary_dim=d, base=10000.0))[0], dtype=torch.float64, device="cuda")
+
+    def plan(self, want, rows):
+        """To the wanted lengths, in place; checked against the oracle."""
+        av = self.av
+        d = av.aurora_cache_plan_desc(batch=self.B, page_size=self.page, max_pages_per_seq=self.width, num_pages=self.P, max_rows=rows)
+        self.positions, self.slots = (torch.empty(rows, dtype=torch.int32, device="cuda") for _ in range(2))
+        self.row_start = torch.empty(self.B + 1, dtype=torch.int32, device="cuda")
+        ref = cache_plan(self.lens.tolist(), want.tolist(), self.table.cpu().numpy(), self.free.cpu().numpy(), int(self.count), self.page, rows)
+        ws = torch.empty(av.aurora_cache_plan_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+        av.aurora_cache_plan(d, self.lens, want, self.table, self.free, self.count, self.count, self.lens, self.row_start, self.positions,
+                             self.slots, None, ws)
+        torch.cuda.synchronize()
+        for got, name in ((self.table, "table"), (self.free, "free"), (self.lens, "seq_lens"), (self.slots, "slots"), (self.positions, "positions")):
+            assert np.array_equal(got.cpu().numpy(), ref[name]), name
+        assert int(self.count) == ref["count"]
+        return ref
+
+    def append(self, qkv):
+        """qkv [rows, (hq + 2 hkv) d]: returns the turned queries."""
+        av, rows = self.av, qkv.shape[0]
+        s = qkv.stride(0)
+        desc = av.aurora_rope_desc(rows=rows, num_q_heads=self.hq, num_kv_heads=self.hkv, head_dim=self.d, rotary_dim=self.d, page_size=self.page,
+                                   num_pages=self.P, dtype=self.code, q_stride=s, k_stride=s, v_stride=s)
+        q, k, v = (x.unflatten(1, (-1, self.d)) for x in qkv.split([self.hq * self.d, self.hkv * self.d, self.hkv * self.d], 1))
+        out = torch.zeros((rows, self.hq, self.d), dtype=self.dt, device="cuda")
+        av.aurora_rope_append(desc, q, k, v, self.positions, self.slots, self.freqs, out, self.kp, self.vp)
+        return out
+
+    def attn_desc(self, nq):
+        return self.av.aurora_attn_desc(batch=self.B, num_q=nq, num_q_heads=self.hq, num_kv_heads=self.hkv, head_dim=self.d, page_size=self.page,
+                                        max_pages_per_seq=self.width, num_pages=self.P, dtype=self.code, sm_scale=0.0)
+
+
+def _dense(q, k, v, n):
+    """Causal attention of the last n of a request's tokens, float64: q [n, hq, d], k and v [L, hkv, d]."""
+    L, G = k.shape[0], q.shape[1] // k.shape[1]
+    k, v = (torch.as_tensor(x).repeat_interleave(G, 1) for x in (k, v))
+    s = torch.einsum("nhd,lhd->hnl", q, k) / math.sqrt(q.shape[2])
+    s = s.masked_fill(torch.arange(L)[None, None] > (L - n + torch.arange(n))[None, :, None], -math.inf)
+    return torch.einsum("hnl,lhd->nhd", torch.softmax(s, -1), v)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_a_server_prefills_verifies_and_rolls_back(gpu_lib, dtype, d):
+    av = gpu_lib
+    B, hq, hkv, page, nq, H, V = 6, 8, 2, 16, 5, 256, 2003
+    torch.manual_seed(3)
+    s = Server(av, B, hq, hkv, d, page, 12, dtype)
+    width = (hq + 2 * hkv) * d
+    prompts = [1, 40, 16, 77, 15, 100]
+    raw = [torch.zeros((0, width), dtype=s.dt) for _ in range(B)]   # every request's tokens, as they were before the rotation
+
+    def feed(rows_of, pad):
+        """The next tokens of every request: one buffer, padded; returns the turned queries."""
+        qkv = torch.randn(sum(rows_of) + pad, width, device="cuda").to(s.dt)
+        at = 0
+        for b, n in enumerate(rows_of):
+            raw[b] = torch.cat([raw[b], qkv[at:at + n].cpu()])
+            at += n
+        return s.append(qkv)
+
+    s.plan(torch.tensor(prompts, dtype=torch.int32, device="cuda"), sum(prompts) + 9)
+    feed(prompts, 9)
+    w = torch.randn(V, H, device="cuda").mul_(0.1).to(s.dt)
+    cd = av.aurora_accept_desc(batch=B, num_q=nq, hidden=H, vocab=V, dtype=s.code, temperature=0.0)
+    for step in range(3):
+        s.plan(s.lens + nq, B * nq)
+        q = feed([nq] * B, 0)
+        ad = s.attn_desc(nq)
+        hidden = torch.randn(B, nq, H, device="cuda").to(s.dt)
+        tokens = torch.randint(0, V, (B, nq), device="cuda", dtype=torch.int32)
+        top = (hidden.float().view(-1, H) @ w.float().T).argmax(1).view(B, nq)
+        for b in range(B):                                     # request b's first b % nq drafts are right
+            n = (b + step) % nq
+            tokens[b, 1:1 + n] = top[b, :n].to(torch.int32)
+        i32 = lambda *z: torch.zeros(z, dtype=torch.int32, device="cuda")
+        alen, nxt, mask, out = i32(B), i32(B), torch.zeros(B, nq, dtype=torch.uint8, device="cuda"), torch.zeros(B, nq, hq, d, dtype=s.dt, device="cuda")
+        ws = torch.empty(av.aurora_verify_workspace_bytes(ad, cd), dtype=torch.uint8, device="cuda")
+        av.aurora_verify(ad, cd, q.view(B, nq, hq, d), s.kp, s.vp, s.table, s.lens, None, out, hidden, w, tokens, None, None, alen, nxt, mask, None,
+                         None, ws)
+        # what is returned with the tokens: the log probability of what followed every position, and three alternatives
+        follow = torch.cat([tokens[:, 1:], nxt[:, None]], 1).contiguous()
+        ld = av.aurora_logprob_desc(rows=B * nq, vocab=V, dtype=av.AURORA_F32, n_top=3)
+        lp, ent, tops, topl = torch.zeros(B * nq, device="cuda"), torch.zeros(B * nq, device="cuda"), i32(B * nq, 3), torch.zeros(B * nq, 3, device="cuda")
+        lws = torch.empty(av.aurora_token_logprobs_workspace_bytes(ld), dtype=torch.uint8, device="cuda")
+        av.aurora_token_logprobs(ld, av.aurora_verify_logits_ptr(ad, cd, ws), follow, lp, ent, None, tops, topl, lws)
+        torch.cuda.synchronize()
+        off = av.aurora_verify_logits_ptr(ad, cd, ws) - ws.data_ptr()
+        logits = ws[off:off + 4 * B * nq * V].view(torch.float32).view(B * nq, V).double().cpu().numpy()
+        ref = token_logprobs(logits, follow.cpu().numpy().reshape(-1), 1.0, 3)
+        assert np.allclose(lp.cpu().numpy(), ref["logprob"], rtol=0, atol=4e-6) and np.array_equal(tops.cpu().numpy(), ref["top_ids"])
+        assert np.allclose(ent.cpu().numpy(), ref["entropy"], atol=1e-5) and np.allclose(topl.cpu().numpy(), ref["top_logprobs"], atol=4e-6)
+        assert (tops.view(B, nq, 3)[:, :, 0].cpu() == top.cpu()).all()
+        lens, freqs = s.lens.tolist(), s.freqs.cpu().numpy()
+        for b in range(B):
+            x = raw[b].double().numpy().reshape(lens[b], -1, d)
+            qkr = rope_turn(x[:, :hq + hkv], np.arange(lens[b]), freqs, d, False)
+            o = _dense(torch.as_tensor(qkr[-nq:, :hq]), torch.as_tensor(qkr[:, hq:]), torch.as_tensor(x[:, hq + hkv:]), nq).numpy()
+            # bfloat16: turned q and k, weights and the output are rounded (2^-8 each, the scores' by |s| of some units); fp32: sums
+            bar = 6e-2 if dtype == "bf16" else 2e-5
+            assert np.abs(out[b].double().cpu().numpy() - o).max() <= bar * max(1.0, np.abs(o).max()), b
+        # only the device knows how much was kept; the rest goes back
+        keep = s.lens - nq + 1 + alen
+        n_keep = keep.tolist()
+        assert [k - (l - nq) - 1 for k, l in zip(n_keep, lens)] == [(b + step) % nq for b in range(B)]
+        s.plan(keep, 4)
+        raw = [r[:n] for r, n in zip(raw, n_keep)]
+    s.plan(torch.zeros_like(s.lens), 0)
+    assert int(s.count) == s.P and sorted(s.free.tolist()) == list(range(s.P))
+
+
+def test_the_gradient_of_projections_through_rotation_and_attention(gpu_lib):
+    """fp32: rope -> attention -> <dout, out>, back to q, k and v, against reverse mode in float64 on the whole chain."""
+    av = gpu_lib
+    B, hq, hkv, d, page, nq = 3, 4, 2, 64, 16, 40
+    torch.manual_seed(4)
+    s = Server(av, B, hq, hkv, d, page, 4, "f32")
+    rows = B * nq
+    s.plan(torch.full((B,), nq, dtype=torch.int32, device="cuda"), rows)
+    s.kp.zero_(), s.vp.zero_()
+    qkv = torch.randn(rows, (hq + 2 * hkv) * d, device="cuda")
+    q = s.append(qkv).view(B, nq, hq, d)
+    ad = s.attn_desc(nq)
+    out, lse, dout = torch.zeros_like(q), torch.zeros(B, nq, hq, device="cuda"), torch.randn_like(q)
+    ws = torch.empty(max(av.aurora_verify_workspace_bytes(ad, None), av.aurora_attn_backward_workspace_bytes(ad)), dtype=torch.uint8, device="cuda")
+    av.aurora_attn_forward(ad, q, s.kp, s.vp, s.table, s.lens, None, out, lse, ws)
+    dq, dkp, dvp = torch.zeros_like(q), torch.zeros_like(s.kp), torch.zeros_like(s.vp)
+    av.aurora_attn_backward_saved(ad, q, s.kp, s.vp, s.table, s.lens, None, out, lse, dout, dq, dkp, dvp, ws)
+    g = torch.zeros_like(qkv)
+    st = g.stride(0)
+    desc = av.aurora_rope_desc(rows=rows, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, rotary_dim=d, page_size=page, num_pages=s.P, dtype=av.AURORA_F32,
+                               q_stride=st, k_stride=st, v_stride=st)
+    gq, gk, gv = (x.unflatten(1, (-1, d)) for x in g.split([hq * d, hkv * d, hkv * d], 1))
+    av.aurora_rope_append_backward(desc, dq.view(rows, hq, d), dkp, dvp, s.positions, s.slots, s.freqs, gq, gk, gv)
+    torch.cuda.synchronize()
+    x = qkv.double().cpu().requires_grad_()
+    h = x.view(B, nq, -1, d)
+    ang = torch.arange(nq, dtype=torch.float64)[:, None] * s.freqs.cpu()
+    c, sn = ang.cos()[:, None], ang.sin()[:, None]
+    a, b = h[..., :d // 2], h[..., d // 2:]
+    turned = torch.cat([a * c - b * sn, b * c + a * sn], -1)
+    o = torch.stack([_dense(turned[i, :, :hq], turned[i, :, hq:hq + hkv], h[i, :, hq + hkv:], nq) for i in range(B)])
+    (o * dout.double().cpu()).sum().backward()
+    # fp32 throughout: sums of up to 40 x 2 x 64 products
+    assert (g.double().cpu() - x.grad).abs().max() <= 2e-5 * x.grad.abs().max()
+
+
+@pytest.mark.parametrize("make", [lambda: gen.tiny_chain(3), lambda: gen.llama_chain(4, batch=3, len_lo=40, len_hi=300, vocab=4099, hidden_size=512)])
+def test_log_probabilities_of_a_step(gpu_lib, make):
+    """The step's own call: what the verified tokens were worth."""
+    from paper_2602_06932_amd.device import DeviceVerify
+    w = make()
+    dv = DeviceVerify(w)
+    dv.verify()
+    dv.trace()
+    dv.logprobs(dv.y_out, n_top=4)
+    torch.cuda.synchronize()
+    logits = dv.logits_host().reshape(-1, w.vocab).astype(np.float64)
+    ref = token_logprobs(logits, dv.y_out.cpu().numpy().reshape(-1), w.temperature, 4)
+    assert np.allclose(dv.logprob.cpu().numpy().reshape(-1), ref["logprob"], atol=4e-6)
+    assert np.allclose(dv.lse.cpu().numpy(), dv.row_lse.cpu().numpy(), atol=4e-6)
+    assert np.array_equal(dv.top_ids.cpu().numpy(), ref["top_ids"])

@@ -1,0 +1,131 @@
+"""Host checks of the calls around the verification step: descriptors, pointers, alignments and workspaces are looked at before any device
+is touched (no address below is ever read)."""
+import pytest
+import torch
+
+import paper_2602_06932_amd as av
+
+P = 4096
+BAD, NOT, WS = av.AURORA_ERR_INVALID_ARG, av.AURORA_ERR_UNSUPPORTED, av.AURORA_ERR_WORKSPACE
+
+
+def _ws(n, short=0):
+    t = torch.empty(n + 256, dtype=torch.uint8)
+    return t[(-t.data_ptr()) % 256:][:n - short]
+
+
+def _desc(kind, base, **kw):
+    return kind(**{**base, **kw})
+
+
+PLAN = dict(batch=3, page_size=16, max_pages_per_seq=8, num_pages=50, max_rows=20)
+PLAN_ARGS = dict(held=P, want=P, table=P, free=P, count=P, count_out=P, lens=P, start=P, positions=P, slots=P, info=P)
+
+
+def _plan(desc={}, ws=None, **kw):
+    d = _desc(av.aurora_cache_plan_desc, PLAN, **desc)
+    return av.aurora_cache_plan(d, *{**PLAN_ARGS, **kw}.values(), ws if ws is not None else _ws(65536), stream=0, check=False)
+
+
+@pytest.mark.parametrize("desc,want", [(dict(batch=-1), BAD), (dict(page_size=0), BAD), (dict(max_pages_per_seq=0), BAD), (dict(num_pages=0), BAD),
+                                       (dict(max_rows=-1), BAD), (dict(num_pages=2 ** 27), NOT), (dict(max_pages_per_seq=2 ** 27), NOT),
+                                       (dict(batch=2 ** 20, max_pages_per_seq=2 ** 12), NOT)])
+def test_plan_descriptors(desc, want):
+    assert _plan(desc) == want
+    with pytest.raises(av.AuroraError):
+        av.aurora_cache_plan_workspace_bytes(_desc(av.aurora_cache_plan_desc, PLAN, **desc))
+
+
+def test_plan_arguments():
+    for name in ("want", "table", "free", "count", "count_out", "lens", "positions", "slots"):
+        assert _plan(**{name: None}) == BAD, name
+    for name in PLAN_ARGS:
+        assert _plan(**{name: P + 2}) == BAD, name
+    n = av.aurora_cache_plan_workspace_bytes(_desc(av.aurora_cache_plan_desc, PLAN))
+    assert _plan(ws=_ws(n, short=1)) == WS and _plan(ws=_ws(n + 8)[8:]) == WS
+    assert av.load().aurora_cache_plan(None, *([None] * 12), 0, None) == BAD
+
+
+ROPE = dict(rows=4, num_q_heads=8, num_kv_heads=2, head_dim=64, rotary_dim=64, page_size=16, num_pages=9, dtype=av.AURORA_BF16)
+ROPE_ARGS = dict(q=P, k=P, v=P, positions=P, slots=P, frequencies=P, q_out=P, kp=P, vp=P)
+
+
+def _rope(desc={}, back=False, **kw):
+    d = _desc(av.aurora_rope_desc, ROPE, **desc)
+    a = {**ROPE_ARGS, **kw}
+    if back:
+        return av.aurora_rope_append_backward(d, a["q_out"], a["kp"], a["vp"], a["positions"], a["slots"], a["frequencies"], a["q"], a["k"], a["v"],
+                                              stream=0, check=False)
+    return av.aurora_rope_append(d, *a.values(), stream=0, check=False)
+
+
+@pytest.mark.parametrize("desc,want", [(dict(rows=-1), BAD), (dict(num_q_heads=-1), BAD), (dict(num_q_heads=0, num_kv_heads=0), BAD), (dict(head_dim=0), BAD),
+                                       (dict(rotary_dim=66), BAD), (dict(rotary_dim=63), BAD), (dict(rotary_dim=-2), BAD), (dict(interleaved=2), BAD),
+                                       (dict(page_size=0), BAD), (dict(num_pages=0), BAD), (dict(dtype=av.AURORA_FP8_E4M3), BAD), (dict(dtype=7), BAD),
+                                       (dict(kv_fp8=1), BAD), (dict(kv_fp8=2), BAD), (dict(magnitude=-1.0), BAD), (dict(magnitude=float("nan")), BAD),
+                                       (dict(magnitude=float("inf")), BAD), (dict(q_stride=511), BAD), (dict(q_out_stride=511), BAD), (dict(k_stride=127), BAD),
+                                       (dict(v_stride=-128), BAD), (dict(head_dim=512), NOT), (dict(rows=2 ** 22 + 1), NOT), (dict(num_pages=2 ** 28), NOT)])
+def test_rope_descriptors(desc, want):
+    assert _rope(desc) == want and _rope(desc, back=True) == want
+
+
+def test_rope_arguments():
+    for back in (False, True):
+        for name in ROPE_ARGS:
+            assert _rope(back=back, **{name: None}) == BAD, name
+        for name in ROPE_ARGS:
+            assert _rope(back=back, **{name: P + 1}) == BAD, name
+        assert _rope(back=back, frequencies=P + 4) == BAD
+        assert _rope(dict(rows=0), back=back, q=None) == av.AURORA_OK
+    assert _rope(dict(dtype=av.AURORA_F32), q=P + 2) == BAD and _rope(back=True, kp=P + 2) == BAD
+    assert _rope(dict(kv_fp8=1, k_scale=P, v_scale=P), back=True) == NOT
+
+
+def test_rows_that_do_not_lie_as_the_descriptor_says():
+    x = torch.zeros(4, 700)
+    d = _desc(av.aurora_rope_desc, ROPE, q_stride=700)
+    with pytest.raises(ValueError):
+        av.aurora_rope_append(_desc(av.aurora_rope_desc, ROPE), x[:, :512], P, P, P, P, P, P, P, P, stream=0, check=False)
+    with pytest.raises(ValueError):
+        av.aurora_rope_append(d, torch.zeros(4, 512), P, P, P, P, P, P, P, P, stream=0, check=False)
+    with pytest.raises(ValueError):
+        av.aurora_rope_append(d, x[:, 0:512:2], P, P, P, P, P, P, P, P, stream=0, check=False)
+
+
+LP = dict(rows=4, vocab=1000, dtype=av.AURORA_F32, n_top=3)
+
+
+def _lp(desc={}, ws=None, **kw):
+    d = _desc(av.aurora_logprob_desc, LP, **desc)
+    a = {**dict(logits=P, tokens=P, logprob=P, entropy=P, lse=P, ids=P, tops=P), **kw}
+    return av.aurora_token_logprobs(d, *a.values(), ws if ws is not None else _ws(1 << 20), stream=0, check=False)
+
+
+def _lpb(desc={}, **kw):
+    d = _desc(av.aurora_logprob_desc, LP, **desc)
+    a = {**dict(logits=P, tokens=P, entropy=P, lse=P, dlogprob=P, dentropy=P, dlogits=P), **kw}
+    return av.aurora_token_logprobs_backward(d, *a.values(), stream=0, check=False)
+
+
+@pytest.mark.parametrize("desc,want", [(dict(rows=-1), BAD), (dict(vocab=0), BAD), (dict(dtype=2), BAD), (dict(n_top=-1), BAD), (dict(row_stride=999), BAD),
+                                       (dict(row_stride=-1), BAD), (dict(temperature=-0.5), BAD), (dict(temperature=float("nan")), BAD),
+                                       (dict(temperature=float("inf")), BAD), (dict(n_top=33), NOT), (dict(vocab=2 ** 24 + 1), NOT)])
+def test_logprob_descriptors(desc, want):
+    assert _lp(desc) == want and _lpb(desc) == want
+    with pytest.raises(av.AuroraError):
+        av.aurora_token_logprobs_workspace_bytes(_desc(av.aurora_logprob_desc, LP, **desc))
+
+
+def test_logprob_arguments():
+    assert _lp(logits=None) == BAD and _lp(tokens=None) == BAD and _lp(logprob=None) == BAD and _lp(ids=None) == BAD and _lp(tops=None) == BAD
+    assert _lp(dict(n_top=0), tokens=None, logprob=None, entropy=None, lse=None) == BAD     # nothing requested
+    for name in ("logits", "tokens", "logprob", "entropy", "lse", "ids", "tops"):
+        assert _lp(**{name: P + 2}) == BAD, name
+    assert _lp(dict(dtype=av.AURORA_BF16), logits=P + 1) == BAD and _lp(dict(temperatures=P + 2)) == BAD
+    n = av.aurora_token_logprobs_workspace_bytes(_desc(av.aurora_logprob_desc, LP, vocab=100000))
+    assert _lp(dict(vocab=100000), ws=_ws(n, short=1)) == WS
+    assert _lp(dict(rows=0), logits=None) == av.AURORA_OK
+    assert _lpb(logits=None) == BAD and _lpb(lse=None) == BAD and _lpb(dlogits=None) == BAD and _lpb(dlogprob=None, dentropy=None) == BAD
+    assert _lpb(tokens=None) == BAD and _lpb(entropy=None) == BAD
+    for name in ("logits", "tokens", "entropy", "lse", "dlogprob", "dentropy", "dlogits"):
+        assert _lpb(**{name: P + 2}) == BAD, name
