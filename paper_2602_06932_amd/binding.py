@@ -195,10 +195,14 @@ def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
     """Device address of a tensor whose rows (dimension 0) may lie apart, as the descriptor's stride says."""
     if t is None or isinstance(t, int):
         return t
-    if not t.is_contiguous() and t.shape[0] > 1 and (t.stride(0) != stride or not t[0].is_contiguous()):
-        raise ValueError(f"{name}: rows are {t.stride(0)} elements apart, the descriptor says {stride or 'contiguous'}")
-    if t.is_contiguous() and stride and t.shape[0] > 1 and t.stride(0) != stride:
-        raise ValueError(f"{name}: rows are {t.stride(0)} elements apart, the descriptor says {stride}")
+    s, n = t.stride(), t.shape
+    dense = 1
+    for k in range(len(n) - 1, 0, -1):
+        if s[k] != dense and n[k] > 1:
+            raise ValueError(f"{name}: the elements of a row must be contiguous")
+        dense *= n[k]
+    if s[0] != (stride or dense) and n[0] > 1:
+        raise ValueError(f"{name}: rows are {s[0]} elements apart, the descriptor says {stride or dense}")
     return t.data_ptr()
 
 

@@ -32,7 +32,10 @@ constexpr int kPlanWaves = kPlanThreads / kWave;
 struct PlanArrays { int32_t *row, *take, *give, *held, *col; };
 struct PlanTotals { int n, freed, taken, rows; };
 
-struct PlanReq { int held, want, col, need, back; int64_t rows; bool grow, shrink, differs; };
+struct PlanReq { int held, want, col, need, back; unsigned rows; bool grow, shrink, differs; };
+
+// Sums of rows stop at 2^32 - 1, past every limit: no order of adding changes them, and one that stopped is refused.
+__device__ __forceinline__ unsigned add_rows(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
 
 __device__ __forceinline__ int pages_of(int tokens, int page) { return (int)(((unsigned)tokens + (unsigned)page - 1u) / (unsigned)page); }
 
@@ -50,34 +53,44 @@ __device__ __forceinline__ PlanReq plan_request(const CachePlanLaunch& P, int b)
   r.col = min(hp, wp);
   r.need = r.grow ? wp - hp : 0;
   r.back = r.shrink ? hp - wp : 0;
-  r.rows = r.grow ? (int64_t)r.want - r.held : 0;
+  r.rows = r.grow ? (unsigned)(r.want - r.held) : 0u;
   return r;
 }
 
-struct PlanSums { int back, need; int64_t rows; };
+struct PlanSums { int back, need; unsigned rows; };
+
+// one step of an inclusive scan over the 64 lanes: adds the sums of the lane that the data-parallel control `kCtl` names
+template <int kCtl, int kRows>
+__device__ __forceinline__ void scan_step(PlanSums& x) {
+  x.back += __builtin_amdgcn_update_dpp(0, x.back, kCtl, kRows, 0xf, false);
+  x.need += __builtin_amdgcn_update_dpp(0, x.need, kCtl, kRows, 0xf, false);
+  x.rows = add_rows(x.rows, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x.rows, kCtl, kRows, 0xf, false));
+}
 
 // exclusive prefix of the threads' sums over the workgroup, and the totals
 __device__ __forceinline__ PlanSums plan_scan(const PlanSums& mine, PlanSums& total, PlanSums* s_wave) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   PlanSums x = mine;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int b = __shfl_up(x.back, o, kWave), n = __shfl_up(x.need, o, kWave);
-    const long long r = __shfl_up((long long)x.rows, o, kWave);
-    if (lane >= o) { x.back += b; x.need += n; x.rows += r; }
-  }
+  scan_step<0x111, 0xf>(x);  // within rows of sixteen: from one, two, four, eight lanes below
+  scan_step<0x112, 0xf>(x);
+  scan_step<0x114, 0xf>(x);
+  scan_step<0x118, 0xf>(x);
+  scan_step<0x142, 0xa>(x);  // the first row's last lane into the second row, the third's into the fourth
+  scan_step<0x143, 0xc>(x);  // the second's into the upper half
   __syncthreads();  // (the last chunk's sums may still be read)
   if (lane == 63) s_wave[wave] = x;
+  PlanSums below = {__shfl_up(x.back, 1, kWave), __shfl_up(x.need, 1, kWave), (unsigned)__shfl_up((int)x.rows, 1, kWave)};
+  if (lane == 0) below = {0, 0, 0u};
   __syncthreads();
-  total = {0, 0, 0};
-  PlanSums before = {0, 0, 0};
+  total = {0, 0, 0u};
+  PlanSums before = {0, 0, 0u};
 #pragma unroll
   for (int w = 0; w < kPlanWaves; ++w) {
     const PlanSums t = s_wave[w];
-    if (w < wave) { before.back += t.back; before.need += t.need; before.rows += t.rows; }
-    total.back += t.back; total.need += t.need; total.rows += t.rows;
+    if (w < wave) { before.back += t.back; before.need += t.need; before.rows = add_rows(before.rows, t.rows); }
+    total.back += t.back; total.need += t.need; total.rows = add_rows(total.rows, t.rows);
   }
-  return {before.back + x.back - mine.back, before.need + x.need - mine.need, before.rows + x.rows - mine.rows};
+  return {before.back + below.back, before.need + below.need, add_rows(before.rows, below.rows)};
 }
 
 // The plan of all requests, by one workgroup; A may lie in LDS (one chunk) or in the workspace.  publish: this workgroup writes
@@ -85,77 +98,82 @@ __device__ __forceinline__ PlanSums plan_scan(const PlanSums& mine, PlanSums& to
 template <bool kOneChunk>
 __device__ __forceinline__ PlanTotals plan_requests(const CachePlanLaunch& P, const PlanArrays& A, bool publish) {
   __shared__ PlanSums s_wave[kPlanWaves];
-  __shared__ int s_cut, s_refused;
-  __shared__ int s_cut_need;
-  __shared__ int64_t s_cut_rows;
+  __shared__ int s_cut, s_refused, s_cut_need;
+  __shared__ unsigned s_cut_rows;
   const int tid = threadIdx.x;
   const int n = min(max(P.free_count[0], 0), P.num_pages);
+  const unsigned most_rows = P.slots ? (unsigned)P.max_rows : UINT32_MAX;
   if (tid == 0) { s_cut = INT32_MAX; s_refused = 0; }
 
   int freed = 0;
   if constexpr (!kOneChunk) {  // the pages given back, before anyone is granted a page
-    PlanSums all = {0, 0, 0};
-    for (int b0 = tid; b0 < P.B; b0 += kPlanThreads) all.back += plan_request(P, b0).back;
-    PlanSums t;
+    PlanSums all = {0, 0, 0u}, t;
+    for (int b = tid; b < P.B; b += kPlanThreads) all.back += plan_request(P, b).back;
     plan_scan(all, t, s_wave);
     freed = t.back;
   }
-  PlanSums carry = {0, 0, 0};
+  PlanSums carry = {0, 0, 0u};
+  int cut = INT32_MAX, cut_need = 0;
+  unsigned cut_rows = 0;
   for (int base = 0; kOneChunk ? base == 0 : base < P.B; base += kPlanChunk) {
     PlanReq r[kPlanPer];
-    PlanSums mine = {0, 0, 0}, total;
+    PlanSums mine = {0, 0, 0u}, total;
+    int refused = 0;
 #pragma unroll
     for (int i = 0; i < kPlanPer; ++i) {
       r[i] = plan_request(P, base + tid * kPlanPer + i);
-      mine.back += r[i].back; mine.need += r[i].need; mine.rows += r[i].rows;
+      mine.back += r[i].back; mine.need += r[i].need; mine.rows = add_rows(mine.rows, r[i].rows);
+      refused += r[i].differs && !r[i].grow && !r[i].shrink;
     }
     PlanSums at = plan_scan(mine, total, s_wave);
     if constexpr (kOneChunk) freed = total.back;
-    at.back += carry.back; at.need += carry.need; at.rows += carry.rows;
-    carry.back += total.back; carry.need += total.need; carry.rows += total.rows;
-    // The sums never fall, so those who are refused for want of pages or rows are one run of growing requests up to the last: the
-    // first of them is all there is to find.
-    PlanSums cum = at;
-    int refused = 0, first = INT32_MAX;
-    PlanSums at_first = {0, 0, 0};
+    at.back += carry.back; at.need += carry.need; at.rows = add_rows(at.rows, carry.rows);
+    carry.back += total.back; carry.need += total.need; carry.rows = add_rows(carry.rows, total.rows);
+    const int64_t pages = (int64_t)n + freed;
+    if (carry.need > pages || carry.rows > most_rows) {  // (the whole workgroup)
+      // The sums never fall, so those who are refused for want of pages or rows are one run of growing requests up to the last: the
+      // first of them is all there is to find.
+      PlanSums cum = at, at_first = {0, 0, 0u};
+      int first = INT32_MAX;
 #pragma unroll
-    for (int i = 0; i < kPlanPer; ++i) {
-      const bool fits = (int64_t)cum.need + r[i].need <= (int64_t)n + freed && (!P.slots || cum.rows + r[i].rows <= P.max_rows);
-      const bool short_of = r[i].grow && !fits;
-      if (short_of && first == INT32_MAX) { first = base + tid * kPlanPer + i; at_first = cum; }
-      refused += short_of || (r[i].differs && !r[i].grow && !r[i].shrink);
-      cum.need += r[i].need; cum.rows += r[i].rows;
+      for (int i = 0; i < kPlanPer; ++i) {
+        const PlanSums next = {0, cum.need + r[i].need, add_rows(cum.rows, r[i].rows)};
+        if (r[i].grow && (next.need > pages || next.rows > most_rows)) {
+          if (first == INT32_MAX) { first = base + tid * kPlanPer + i; at_first = cum; }
+          ++refused;
+        }
+        cum = next;
+      }
+      if (first != INT32_MAX) atomicMin(&s_cut, first);
+      __syncthreads();
+      if (first != INT32_MAX && s_cut == first) { s_cut_need = at_first.need; s_cut_rows = at_first.rows; }
+      __syncthreads();
+      cut = s_cut; cut_need = s_cut_need; cut_rows = s_cut_rows;
     }
-    if (first != INT32_MAX) atomicMin(&s_cut, first);
     if (refused) atomicAdd(&s_refused, refused);
-    __syncthreads();
-    if (first != INT32_MAX && s_cut == first) { s_cut_need = at_first.need; s_cut_rows = at_first.rows; }
-    __syncthreads();
-    const int cut = s_cut;
-    cum = at;
+    PlanSums cum = at;
 #pragma unroll
     for (int i = 0; i < kPlanPer; ++i) {
       const int b = base + tid * kPlanPer + i;
       if (b < P.B) {
         const bool past = b >= cut;
-        const int row = (int)(past ? s_cut_rows : cum.rows), take = past ? s_cut_need : cum.need;
-        A.row[b] = row; A.take[b] = take; A.give[b] = cum.back; A.held[b] = r[i].held; A.col[b] = r[i].col;
+        const int row = (int)(past ? cut_rows : cum.rows);
+        A.row[b] = row; A.take[b] = past ? cut_need : cum.need; A.give[b] = cum.back; A.held[b] = r[i].held; A.col[b] = r[i].col;
         if (publish) {
           P.seq_lens[b] = r[i].shrink || (r[i].grow && !past) ? r[i].want : r[i].held;
           if (P.row_start) P.row_start[b] = row;
         }
       }
-      cum.back += r[i].back; cum.need += r[i].need; cum.rows += r[i].rows;
+      cum.back += r[i].back; cum.need += r[i].need; cum.rows = add_rows(cum.rows, r[i].rows);
     }
   }
-  if constexpr (!kOneChunk) __syncthreads();
   PlanTotals t;
-  const bool cut = s_cut != INT32_MAX;
   t.n = n;
   t.freed = freed;
-  t.taken = cut ? s_cut_need : carry.need;
-  t.rows = (int)(cut ? s_cut_rows : carry.rows);
+  t.taken = cut != INT32_MAX ? cut_need : carry.need;
+  t.rows = (int)(cut != INT32_MAX ? cut_rows : carry.rows);
   if (tid == 0) { A.row[P.B] = t.rows; A.take[P.B] = t.taken; A.give[P.B] = t.freed; }
+  __syncthreads();
   if (publish && tid == 0) {
     if (P.row_start) P.row_start[P.B] = t.rows;
     P.free_count_out[0] = (int)min((int64_t)n + freed - t.taken, (int64_t)P.num_pages);
@@ -164,12 +182,15 @@ __device__ __forceinline__ PlanTotals plan_requests(const CachePlanLaunch& P, co
   return t;
 }
 
-// the request whose run of `start` holds x: the last b with start[b] <= x (start[0] = 0, x < start[B])
+// the request whose run of `start` holds x: the last b with start[b] <= x (start[0] = 0, x < start[B]); a quarter of the range a step
 __device__ __forceinline__ int plan_owner(const int32_t* start, int B, int x) {
-  int lo = 0, hi = B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (start[mid] <= x) lo = mid; else hi = mid - 1;
+  int lo = 0, n = B;
+  while (n > 1) {
+    const int q = (n + 3) >> 2;  // the pieces start at lo, lo + q, lo + 2q, lo + 3q
+    const int a = start[lo + min(q, n)], b = start[lo + min(2 * q, n)], c = start[lo + min(3 * q, n)];
+    const int piece = (a <= x) + (b <= x) + (c <= x);
+    lo += piece * q;
+    n = min(q, n - piece * q);
   }
   return lo;
 }
@@ -234,7 +255,6 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanLaunc
   __shared__ int32_t s_row[kPlanChunk + 1], s_take[kPlanChunk + 1], s_give[kPlanChunk + 1], s_held[kPlanChunk], s_col[kPlanChunk];
   const PlanArrays A = {s_row, s_take, s_give, s_held, s_col};
   const PlanTotals t = plan_requests<true>(P, A, blockIdx.x == 0);
-  __syncthreads();
   plan_write(P, A, t);
 }
 

@@ -183,9 +183,9 @@ struct RopeLaunch {
   // in: rows of q, k and v, and where they go.  Back: q, k and v are the gradients' rows, written; q_out and the pools are read, fp32
   const void *q, *k, *v;
   void *q_out, *k_pages, *v_pages;
-  int block_rows;                                          // set by the launcher
+  int block_rows, chunks, page_shift;                                  // set by the launcher
 };
-constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;   // what the launch's second dimension and a block's angles in LDS allow
+constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;   // so that a block's angles fit into LDS
 hipError_t launch_rope(const RopeLaunch& P, bool back, hipStream_t st);
 
 // log probabilities of given tokens, entropy, alternatives, and the gradient (see logprob.hip)

@@ -23,13 +23,13 @@
 
 namespace aurora {
 
-constexpr int kLpThreads = 512;
+constexpr int kLpThreads = 256;
 constexpr int kLpWaves = kLpThreads / kWave;
 constexpr int kLpVecs = 4;                              // 16-byte vectors of a thread in one step
 constexpr int kLpStep = kLpThreads * kLpVecs;           // vectors of a step
-constexpr int kLpMaxSteps = 32;                         // steps of a workgroup: bounds the block maxima in LDS
+constexpr int kLpMaxSteps = 64;                         // steps of a workgroup: bounds the block maxima in LDS
 constexpr int kLpLanes = 8;                             // lanes that share a block: 128 bytes a load
-constexpr int kLpGroups = kLpThreads / kLpLanes;
+constexpr int kLpGroups = kLpThreads / kLpLanes;        // columns of blocks: at least kLpMaxTop of them
 constexpr int kLpBlocks = kLpMaxSteps * kLpGroups;      // and one for the elements outside whole vectors
 constexpr int kLpList = 512;
 constexpr int kLpMaxTop = 32;
@@ -126,6 +126,7 @@ __device__ __forceinline__ float lp_scale(const LogprobLaunch& P, size_t row) { 
 // ---- selection of the n largest of a workgroup's part -------------------------------------------------------------------
 struct LpLds {
   float bm[kLpBlocks + 1];            // block maxima; the last one is of the elements outside whole vectors
+  float col[kLpGroups];               // and the maxima of their columns
   unsigned short blocks[kLpBlocks + 1];
   unsigned long long list[kLpList];
   int cnt[16][4];
@@ -181,25 +182,38 @@ __device__ __forceinline__ bool lp_element(const T* row, const LpPart& w, int bl
   return true;
 }
 
-// Lists what the blocks in L.blocks hold above the bound (or at it, with_ties); stops once the list is past its size.  Returns how
-// many there are, kLpList + 1 if too many.
+// Lists what the blocks in L.blocks hold above the bound (or at it, with_ties), a vector a thread at a time; stops once the list is past
+// its size.  Returns how many there are, kLpList + 1 if too many.
 template <typename T>
 __device__ __forceinline__ int lp_gather(const T* row, const LpPart& w, unsigned bound, bool with_ties, LpLds& L) {
-  constexpr int kBlock = LpType<T>::kV * kLpLanes * kLpVecs;
+  constexpr int kV = LpType<T>::kV, kPer = kLpLanes * kLpVecs;
   __syncthreads();
   if (threadIdx.x == 0) L.n_list = 0;
   __syncthreads();
-  const int all = L.n_blocks * kBlock;
-  for (int i = threadIdx.x; i < all; i += kLpThreads) {
-    if (*(volatile int*)&L.n_list > kLpList) break;
-    int id;
-    float z;
-    if (!lp_element(row, w, L.blocks[i / kBlock], i % kBlock, id, z)) continue;
+  auto offer = [&](float z, int id) {
     const unsigned o = lp_order(z);
     if (o > bound || (with_ties && o == bound)) {
       const int at = atomicAdd(&L.n_list, 1);
       if (at < kLpList) L.list[at] = lp_key(z, id);
     }
+  };
+  const int all = L.n_blocks * kPer;
+  for (int i = threadIdx.x; i < all; i += kLpThreads) {
+    if (*(volatile int*)&L.n_list > kLpList) break;
+    const int blk = L.blocks[i / kPer], u = i % kPer;
+    if (blk == kLpBlocks) {  // outside whole vectors: less than a vector's elements before, and after them
+      int id;
+      float z;
+      if (u < 2 * kV && lp_element(row, w, blk, u, id, z)) offer(z, id);
+      continue;
+    }
+    const int vec = blk / kLpGroups * kLpStep + u / kLpLanes * kLpThreads + blk % kLpGroups * kLpLanes + u % kLpLanes;
+    if (vec >= w.vecs) continue;
+    const int id = w.first + vec * kV;
+    float x[kV];
+    lp_widen<T>(*(const u32x4_t*)(row + id), x);
+#pragma unroll
+    for (int e = 0; e < kV; ++e) offer(x[e], id + e);
   }
   __syncthreads();
   return min(L.n_list, kLpList + 1);
@@ -223,25 +237,38 @@ template <typename T, typename Out>
 __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int n, LpLds& L, Out out) {
   constexpr int kV = LpType<T>::kV, kBlock = kV * kLpLanes * kLpVecs;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int used = w.steps * kLpGroups;
+  // The n-th largest column maximum: as good a bound for most rows, and one wavefront finds it by counting, without a barrier.
   unsigned bound;
   {
-    constexpr int kPer = (kLpBlocks + kLpThreads - 1) / kLpThreads;
-    unsigned v[kPer + 1];
+    static_assert(kLpGroups <= kWave && kLpGroups >= kLpMaxTop, "a column a lane");
+    const unsigned mine = lane < kLpGroups ? lp_order(L.col[lane]) : 0u;
+    int above = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = tid + i * kLpThreads < used ? lp_order(L.bm[tid + i * kLpThreads]) : 0u;
-    v[kPer] = tid == 0 ? lp_order(L.bm[kLpBlocks]) : 0u;
-    bound = lp_nth(v, n, L);
+    for (int i = 0; i < kLpGroups; ++i) {
+      const unsigned other = __builtin_amdgcn_readlane(mine, i);
+      above += other > mine || (other == mine && i < lane);
+    }
+    bound = __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)__ballot(above == n - 1)) - 1);
   }
   lp_blocks(w.steps, bound, false, L);
   int count = lp_gather(row, w, bound, true, L);
   bool ties = false;  // the equal ones are still to be found
   if (count > kLpList) {
+    // The n-th largest block maximum is closer, and less than n blocks are above it.
+    const int used = w.steps * kLpGroups;
+    {
+      constexpr int kPer = (kLpBlocks + kLpThreads - 1) / kLpThreads;
+      unsigned v[kPer + 1];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[i] = tid + i * kLpThreads < used ? lp_order(L.bm[tid + i * kLpThreads]) : 0u;
+      v[kPer] = tid == 0 ? lp_order(L.bm[kLpBlocks]) : 0u;
+      bound = lp_nth(v, n, L);
+    }
     lp_blocks(w.steps, bound, true, L);
     count = lp_gather(row, w, bound, false, L);
     ties = true;
     if (count > kLpList) {
-      // At most n - 1 blocks are above the bound, and they hold more than the list: the n-th largest element is among theirs.
+      // They hold more than the list: the n-th largest element is among theirs.
       constexpr int kPer = (kLpMaxTop * kBlock + kLpThreads - 1) / kLpThreads;
       unsigned v[kPer];
 #pragma unroll
@@ -311,9 +338,10 @@ __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int n, 
 
 // ---- forward --------------------------------------------------------------------------------------------------------------
 template <typename T, bool kTop>
-__global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaunch P) {
+__global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch P) {
   constexpr int kV = LpType<T>::kV;
   __shared__ LpSums s_part[kLpWaves];
+  __shared__ float s_m[kLpWaves];
   __shared__ double s_lse2;
   __shared__ typename std::conditional<kTop, LpLds, int>::type s_lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -328,15 +356,16 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
   u32x4_t cur[kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
 #pragma unroll
-    for (int u = 0; u < kLpVecs; ++u) v[u] = vp[max(0, min(step * kLpStep + u * kLpThreads + tid, w.vecs - 1))];
+    for (int u = 0; u < kLpVecs; ++u) v[u] = __builtin_nontemporal_load(vp + min(step * kLpStep + u * kLpThreads + tid, w.vecs - 1));
   };
-  if (w.vecs > 0) load(0, cur);
+  if (w.steps > 0) load(0, cur);
   const float c = lp_scale(P, row);
   const int token = P.tokens ? P.tokens[row] : -1;
   const bool known = token >= 0 && token < P.V;
   const float z_t = known ? to_f32<T>(z[token]) : 0.f;
 
   LpSums mine = {-INFINITY, 0.0, 0.0};
+  float col = -INFINITY;
   float neg = 0.f;  // minus the reference
   bool far = false;
   // takes elements into the running sums (top: their maximum)
@@ -387,6 +416,7 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
       top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x4E, 0xf, 0xf, true)));
       top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x141, 0xf, 0xf, true)));
       if (tid % kLpLanes == 0) s_lds.bm[step * kLpGroups + tid / kLpLanes] = top;
+      col = fmaxf(col, top);
     }
   };
   for (int step = 0; step < w.steps; ++step) {
@@ -407,27 +437,28 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
         top = wave_max(top);
         if (lane == 0) s_lds.bm[kLpBlocks] = top;
       }
+      if (tid % kLpLanes == 0) s_lds.col[tid / kLpLanes] = col;
     }
   }
 
   // ---- the workgroup's sums ------------------------------------------------------------------------------------
   {
-    const float m = wave_max(mine.m);
+    float m = wave_max(mine.m);
+    if (lane == 0) s_m[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kLpWaves; ++i) m = fmaxf(m, s_m[i]);
     mine = lp_moved(mine, m, c);
     const double s = wave_sum(mine.s), t = wave_sum(mine.t);
     if (lane == 0) s_part[wave] = {m, s, t};
   }
   __syncthreads();
   if (tid == 0) {
-    float m = s_part[0].m;
+    LpSums all = s_part[0];
 #pragma unroll
-    for (int i = 1; i < kLpWaves; ++i) m = fmaxf(m, s_part[i].m);
-    LpSums all = {m, 0.0, 0.0};
-#pragma unroll
-    for (int i = 0; i < kLpWaves; ++i) {
-      const LpSums x = lp_moved(s_part[i], m, c);
-      all.s += x.s;
-      all.t += x.t;
+    for (int i = 1; i < kLpWaves; ++i) {
+      all.s += s_part[i].s;
+      all.t += s_part[i].t;
     }
     if (P.splits == 1) s_lse2 = lp_finish(P, row, all, c, z_t, known);
     else P.parts[task] = LogprobPart{all.s, all.t, all.m, 0.f};
@@ -437,9 +468,8 @@ __global__ __launch_bounds__(kLpThreads, 4) void logprob_rows_kernel(LogprobLaun
       unsigned long long* keys = P.keys + (size_t)task * P.n_top;
       lp_select(z, w, P.n_top, s_lds, [&](int rank, unsigned long long k) { keys[rank] = k; });
     } else {
-      __syncthreads();
-      const double base = s_lse2;
       lp_select(z, w, P.n_top, s_lds, [&](int rank, unsigned long long k) {
+        const double base = s_lse2;  // (the selection has barriers of its own)
         const float v = lp_value((unsigned)(k >> 32));
         const size_t at = row * P.n_top + rank;
         P.top_ids[at] = k ? (int32_t)(0xffffffffu - (unsigned)k) : -1;
@@ -476,7 +506,11 @@ __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobL
     if (n > 0) {
       const unsigned long long head = tid < parts ? P.keys[(row * parts + tid) * n] : 0ull;
       int above = 0;
-      for (int i = 0; i < parts; ++i) above += __shfl(head, i, kWave) > head;
+      for (int i = 0; i < parts; ++i) {
+        const unsigned long long other = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(head >> 32), i) << 32 |
+                                         (unsigned)__builtin_amdgcn_readlane((int)head, i);
+        above += other > head;
+      }
       if (tid == 0) { s_n = 0; s_bound = 0; }
       if (above == n - 1 && head) s_bound = head;  // (keys are distinct)
     }
@@ -545,7 +579,7 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
   for (int v0 = 0; v0 < w.vecs; v0 += kLpBackThreads * kLpBackVecs) {
     u32x4_t raw[kLpBackVecs];
 #pragma unroll
-    for (int u = 0; u < kLpBackVecs; ++u) raw[u] = vp[min(v0 + u * kLpBackThreads + tid, w.vecs - 1)];
+    for (int u = 0; u < kLpBackVecs; ++u) raw[u] = __builtin_nontemporal_load(vp + min(v0 + u * kLpBackThreads + tid, w.vecs - 1));
 #pragma unroll
     for (int u = 0; u < kLpBackVecs; ++u) {
       const int vec = v0 + u * kLpBackThreads + tid;
@@ -566,7 +600,7 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
         else o[i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{x[2 * i], x[2 * i + 1]}), bf16x2_t));
       }
       if (P.wide) {
-        *(u32x4_t*)(g + id) = o;
+        __builtin_nontemporal_store(o, (u32x4_t*)(g + id));
       } else {  // the gradient's rows start elsewhere within 16 bytes than the logits'
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -588,14 +622,14 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
-// Workgroups per row: one where the rows fill the chip (256 compute units, two to four workgroups each), else as many as do, of no less than
-// a step's quarter; and never more than a workgroup's block maxima allow.
+// Workgroups per row: one where the rows fill the chip (256 compute units, several workgroups each), else as many as do, of no less than
+// two steps; and never more than a workgroup's block maxima allow.
 int logprob_splits(int64_t rows, int V, bool bf16) {
   const int per_vec = bf16 ? 8 : 4;
   const int64_t vecs = V / per_vec;
   const int64_t least = (vecs + (int64_t)kLpStep * kLpMaxSteps - 1) / ((int64_t)kLpStep * kLpMaxSteps);
-  int64_t want = rows >= 512 ? 1 : (767 + rows) / rows;
-  want = std::min<int64_t>(want, vecs / kLpThreads);
+  int64_t want = rows >= 1024 ? 1 : (1279 + rows) / std::max<int64_t>(rows, 1);
+  want = std::min<int64_t>(want, vecs / (2 * kLpStep));
   want = std::min<int64_t>(want, kLpMaxSplits);
   return (int)std::max<int64_t>(std::max<int64_t>(want, least), 1);
 }

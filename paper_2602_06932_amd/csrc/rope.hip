@@ -19,7 +19,8 @@
 
 namespace aurora {
 
-constexpr int kRopeThreads = 128;
+constexpr int kRopeThreads = 192;
+constexpr int kRopeAhead = 2;  // rows on their way, and of a block where there are many
 
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
@@ -89,14 +90,15 @@ template <typename T, typename TC, bool kPairs, int kN, bool kBack>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
   extern __shared__ __attribute__((aligned(16))) f32x2_t s_turn[];  // [rows of the block][R / 2] (cos, sin)
   const int tid = threadIdx.x, half = P.rotary / 2;
-  const int row0 = blockIdx.y * P.block_rows, rows = min(P.block_rows, P.rows - row0);
+  const int block = blockIdx.x / P.chunks, chunk = blockIdx.x - block * P.chunks;
+  const int row0 = block * P.block_rows, rows = min(P.block_rows, P.rows - row0);
 
   // ---- this thread's unit ------------------------------------------------------------------------------------
   const int turning = half / kN;                                        // units of a head that are turned
   const int passing = (P.D - P.rotary + 2 * kN - 1) / (2 * kN);         // that pass through
   const int per_head = turning + passing, per_value = (P.D + 2 * kN - 1) / (2 * kN);
   const int rotated = (P.Hq + P.Hkv) * per_head;
-  const int unit = blockIdx.x * kRopeThreads + tid;
+  const int unit = chunk * kRopeThreads + tid;
   const bool used = unit < rotated + P.Hkv * per_value;
   bool turns = false, two = true;
   int head, e0, e1, pair = 0;  // the unit's vectors start at elements e0 and e1 of the head
@@ -123,6 +125,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
   const bool is_q = head < P.Hq, is_v = head >= P.Hq + P.Hkv;
   const int hk = is_q ? 0 : head - P.Hq - (is_v ? P.Hkv : 0);
   if (!two) e1 = e0;
+  const bool side = two && e1 == e0 + kN && P.D % (2 * kN) == 0;  // side by side, at an even vector of the pool
 
   // rows side: q, k or v of a token (read on the way in, written on the way back); the other side: the rotated q's row, or the cache
   T* rows_p = (T*)(is_q ? P.q : is_v ? P.v : P.k);
@@ -140,11 +143,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
   // where row r's part of the other side is, or -1: a row behind the last sequence
   auto slot_of = [&](int r) -> int {
     if (!P.slots) return 0;
-    const int s = P.slots[row0 + r];
+    const int s = __builtin_amdgcn_readfirstlane(P.slots[row0 + r]);
     return s >= 0 && s < P.num_slots ? s : -1;
   };
   auto pool_at = [&](int slot) -> int64_t {
-    const int page = slot / P.page;
+    const int page = P.page_shift >= 0 ? slot >> P.page_shift : slot / P.page;
     return (((int64_t)page * P.Hkv + hk) * P.page + (slot - page * P.page)) * P.D;
   };
   auto load = [&](int r, int slot, float (&a)[kN], float (&b)[kN]) {
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
     }
   };
 
-  constexpr int kAhead = 2;  // rows on their way
+  constexpr int kAhead = kRopeAhead;
   float xa[kAhead][kN], xb[kAhead][kN];
   int slot[kAhead];
 #pragma unroll
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
   // ---- the block's angles ------------------------------------------------------------------------------------
   for (int i = tid; i < rows * half; i += kRopeThreads) {
     const int r = i / half, p = i - r * half;
-    const double turn = (double)P.positions[row0 + r] * P.frequencies[p] * 0.15915494309189533577;  // / 2 pi
+    const double turn = (double)P.positions[row0 + r] * (P.frequencies[p] * 0.15915494309189533577);  // / 2 pi
     const double part = turn - rint(turn);
     const float hi = (float)(2.0 * part), lo = (float)(2.0 * part - (double)hi);  // half turns
     float s, c;
@@ -240,8 +243,13 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
               for (int e = 0; e < kN; ++e) { a[e] = a[e] / scale; b[e] = b[e] / scale; }
             }
             TC* p = (TC*)pool + pool_at(sl);
-            store_vec<kN>(p + e0, a);
-            if (two) store_vec<kN>(p + e1, b);
+            if (sizeof(TC) == 1 && kN == 8 && side) {  // sixteen codes side by side in one store
+              *(u32x4_t*)(p + e0) = u32x4_t{e4m3_pack4(a[0], a[1 % kN], a[2 % kN], a[3 % kN]), e4m3_pack4(a[4 % kN], a[5 % kN], a[6 % kN], a[7 % kN]),
+                                            e4m3_pack4(b[0], b[1 % kN], b[2 % kN], b[3 % kN]), e4m3_pack4(b[4 % kN], b[5 % kN], b[6 % kN], b[7 % kN])};
+            } else {
+              store_vec<kN>(p + e0, a);
+              if (two) store_vec<kN>(p + e1, b);
+            }
           }
         }
       }
@@ -253,15 +261,16 @@ template <typename T, typename TC, bool kPairs, int kN, bool kBack>
 static hipError_t launch_rope_k(RopeLaunch P, hipStream_t st) {
   const int half = P.rotary / 2;
   const int units = (P.Hq + P.Hkv) * (half / kN + (P.D - P.rotary + 2 * kN - 1) / (2 * kN)) + P.Hkv * ((P.D + 2 * kN - 1) / (2 * kN));
-  const int gx = (units + kRopeThreads - 1) / kRopeThreads;
-  // rows of a block: few while the launch would not fill the chip, then as many as share the cost of a block's start
-  int rows = 1;
-  while (rows < 8 && (int64_t)gx * (P.rows / (2 * rows)) >= 2048) rows *= 2;
-  while ((P.rows + rows - 1) / rows > 65535) rows *= 2;  // (the grid's second dimension)
-  P.block_rows = rows;
+  P.page_shift = (P.page & (P.page - 1)) == 0 ? __builtin_ctz(P.page) : -1;
+  P.chunks = (units + kRopeThreads - 1) / kRopeThreads;
+  // One row a block while the launch would not fill the chip, then as many as are loaded ahead: more only make a block's start longer
+  // (two a block, four, eight, sixteen: 16384 rows of 32 + 8 + 8 heads of 128 77, 77, 82, 99 us, their gradients 54.5, 58.5, 63, 63).
+  int64_t rows = (int64_t)P.chunks * P.rows / kRopeAhead >= 2048 ? kRopeAhead : 1;
+  while ((P.rows + rows - 1) / rows * P.chunks > ((int64_t)1 << 32) / kRopeThreads - 1) rows *= 2;  // fewer than 2^32 threads
+  P.block_rows = (int)rows;
   const size_t lds = (size_t)rows * half * sizeof(f32x2_t);
   if (lds > 64 * 1024) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((rope_kernel<T, TC, kPairs, kN, kBack>), dim3(gx, (P.rows + rows - 1) / rows), dim3(kRopeThreads), lds, st, P);
+  hipLaunchKernelGGL((rope_kernel<T, TC, kPairs, kN, kBack>), dim3((unsigned)((P.rows + rows - 1) / rows * P.chunks)), dim3(kRopeThreads), lds, st, P);
   return hipGetLastError();
 }
 
