@@ -182,8 +182,8 @@ def status_string(status: int) -> str:
 
 def _ptr(t) -> Optional[int]:
     """Device address of a torch tensor (or a raw integer address, or None)."""
-    if t is None:
-        return None
+    if t is None or t.__class__ is int:
+        return t
     if isinstance(t, int):
         return t
     if not t.is_contiguous():
@@ -193,10 +193,14 @@ def _ptr(t) -> Optional[int]:
 
 def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
     """Device address of a tensor whose rows (dimension 0) may lie apart, as the descriptor's stride says."""
-    if t is None or isinstance(t, int):
+    if t is None or t.__class__ is int:
         return t
-    s, n = t.stride(), t.shape
-    dense = 1
+    s = t.stride()
+    if s[0] == stride and len(s) == 3 and s[2] == 1 and s[1] == t.size(2):  # what a view of a fused projection's output is
+        return t.data_ptr()
+    if stride == 0 and t.is_contiguous():
+        return t.data_ptr()
+    n, dense = t.shape, 1
     for k in range(len(n) - 1, 0, -1):
         if s[k] != dense and n[k] > 1:
             raise ValueError(f"{name}: the elements of a row must be contiguous")
@@ -206,10 +210,24 @@ def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
     return t.data_ptr()
 
 
+_current = None  # the current stream's handle, by the shortest way that the installed torch has
+
+
+def _find_current():
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.current_stream()  # (initialises the device)
+    return lambda: raw(device())
+
+
 def _stream(stream) -> Optional[int]:
+    global _current
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _current is None:
+            _current = _find_current()
+        return _current()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
