@@ -189,7 +189,7 @@ constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;   // so that a block's 
 hipError_t launch_rope(const RopeLaunch& P, bool back, hipStream_t st);
 
 // log probabilities of given tokens, entropy, alternatives, and the gradient (see logprob.hip)
-struct LogprobPart { double s, t; float m, pad; };
+struct LogprobPart { double s, t; float m, z_t; };  // (z_t: the token's logit, the same in all parts of a row)
 struct LogprobLaunch {
   int rows, V, n_top;
   bool bf16, wide;

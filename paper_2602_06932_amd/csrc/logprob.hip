@@ -23,15 +23,20 @@
 
 namespace aurora {
 
-constexpr int kLpThreads = 256;
-constexpr int kLpWaves = kLpThreads / kWave;
-constexpr int kLpVecs = 4;                              // 16-byte vectors of a thread in one step
-constexpr int kLpStep = kLpThreads * kLpVecs;           // vectors of a step
-constexpr int kLpMaxSteps = 64;                         // steps of a workgroup: bounds the block maxima in LDS
-constexpr int kLpLanes = 8;                             // lanes that share a block: 128 bytes a load
-constexpr int kLpGroups = kLpThreads / kLpLanes;        // columns of blocks: at least kLpMaxTop of them
-constexpr int kLpBlocks = kLpMaxSteps * kLpGroups;      // and one for the elements outside whole vectors
-constexpr int kLpList = 512;
+constexpr int kLpVecs = 4;  // 16-byte vectors of a thread in one step
+// What a workgroup of kT threads takes: a step is kT * kLpVecs vectors of the row; a block is the kLanes lanes' vectors of one step, and
+// the same lanes' blocks of all steps are one of 64 columns.
+template <int kT>
+struct LpShape {
+  static constexpr int kThreads = kT, kWaves = kT / kWave;
+  static constexpr int kStep = kT * kLpVecs;
+  static constexpr int kColumns = kWave, kLanes = kT / kColumns;
+  static constexpr int kMaxSteps = kT == 256 ? 64 : 16;  // bounds the block maxima in LDS
+  static constexpr int kBlocks = kMaxSteps * kColumns;   // and one for the elements outside whole vectors
+  static constexpr int kList = kT == 256 ? 512 : 256;    // elements, and blocks, that are ranked by counting
+};
+typedef LpShape<256> LpWide;    // long rows
+typedef LpShape<64> LpNarrow;   // short rows: a wavefront each
 constexpr int kLpMaxTop = 32;
 constexpr int kLpMaxSplits = 64;
 constexpr float kLpLog2e = 1.4426950408889634f;
@@ -70,7 +75,7 @@ __device__ __forceinline__ unsigned long long lp_key(float z, int id) {
 
 // The part [lo, hi) of a row that a workgroup takes: `vecs` whole vectors from element `first` on, up to kV - 1 elements before them and
 // as many after.
-struct LpPart { int lo, first, vecs, tail, hi, steps; };
+struct LpPart { int lo, first, vecs, tail, hi; };
 template <typename T>
 __device__ __forceinline__ LpPart lp_part(const T* row, int V, int split, int splits) {
   constexpr int kV = LpType<T>::kV;
@@ -83,7 +88,6 @@ __device__ __forceinline__ LpPart lp_part(const T* row, int V, int split, int sp
   p.tail = p.first + p.vecs * kV;
   p.lo = split == 0 ? 0 : p.first;
   p.hi = split == splits - 1 ? V : p.tail;
-  p.steps = (p.vecs + kLpStep - 1) / kLpStep;
   return p;
 }
 
@@ -123,21 +127,36 @@ __device__ __forceinline__ float lp_temperature(const LogprobLaunch& P, size_t r
 }
 __device__ __forceinline__ float lp_scale(const LogprobLaunch& P, size_t row) { return kLpLog2e / lp_temperature(P, row); }
 
+// how many of the list are larger, eight reads at a time (one at a time each waits for the last: 256 keys 12 us)
+constexpr int kLpRankStep = 8;
+__device__ __forceinline__ int lp_rank(const unsigned long long* list, int count, unsigned long long k) {
+  int rank = 0;
+  for (int j = 0; j < count; j += kLpRankStep) {
+    unsigned long long other[kLpRankStep];
+#pragma unroll
+    for (int e = 0; e < kLpRankStep; ++e) other[e] = list[j + e];
+#pragma unroll
+    for (int e = 0; e < kLpRankStep; ++e) rank += other[e] > k;
+  }
+  return rank;
+}
+
 // ---- selection of the n largest of a workgroup's part -------------------------------------------------------------------
+template <typename S>
 struct LpLds {
-  float bm[kLpBlocks + 1];            // block maxima; the last one is of the elements outside whole vectors
-  float col[kLpGroups];               // and the maxima of their columns
-  unsigned short blocks[kLpBlocks + 1];
-  unsigned long long list[kLpList];
+  float bm[S::kBlocks + 1];           // block maxima; the last one is of the elements outside whole vectors
+  float col[S::kColumns];             // and the maxima of their columns
+  unsigned short blocks[S::kList];
+  unsigned long long list[S::kList + kLpRankStep];  // (zeros behind the last)
   int cnt[16][4];
   int n_blocks, n_list;
-  int best[kLpWaves];
+  int best[S::kWaves];
 };
 
-// The largest bound that at least n of the workgroup's values reach (thread t holds kPer of them, as lp_order keys; 0: no value):
-// two bits at a time from the top.  0 if there are fewer than n.
-template <int kPer>
-__device__ __forceinline__ unsigned lp_nth(const unsigned (&v)[kPer], int n, LpLds& L) {
+// The largest bound that at least n of `count` values reach (value(i): an lp_order key, or 0 for none): two bits at a time from the top.
+// 0 if there are fewer than n.
+template <typename S, typename Value>
+__device__ __forceinline__ unsigned lp_nth(int count, int n, LpLds<S>& L, Value value) {
   const int tid = threadIdx.x, lane = tid & 63;
   __syncthreads();
   if (tid < 64) L.cnt[tid >> 2][tid & 3] = 0;
@@ -147,11 +166,11 @@ __device__ __forceinline__ unsigned lp_nth(const unsigned (&v)[kPer], int n, LpL
   for (int step = 0; step < 16; ++step) {
     const int sh = 30 - 2 * step;
     int c[3] = {0, 0, 0};
+#pragma unroll 1
+    for (int i = tid; i - tid < count; i += S::kThreads) {
+      const unsigned v = i < count ? value(i) : 0u;
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      const unsigned bound = p | (unsigned)(q + 1) << sh;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) c[q] += __popcll(__ballot(v[i] >= bound));
+      for (int q = 0; q < 3; ++q) c[q] += __popcll(__ballot(v >= (p | (unsigned)(q + 1) << sh)));
     }
     if (lane < 3) {
       const int mine = lane == 0 ? c[0] : lane == 1 ? c[1] : c[2];
@@ -165,16 +184,16 @@ __device__ __forceinline__ unsigned lp_nth(const unsigned (&v)[kPer], int n, LpL
 }
 
 // element `i` of block `blk` in the order lane, vector, element - and whether there is one
-template <typename T>
+template <typename S, typename T>
 __device__ __forceinline__ bool lp_element(const T* row, const LpPart& w, int blk, int i, int& id, float& z) {
   constexpr int kV = LpType<T>::kV;
-  if (blk == kLpBlocks) {  // outside whole vectors
+  if (blk == S::kBlocks) {  // outside whole vectors
     const int before = w.first - w.lo;
     id = i < before ? w.lo + i : w.tail + i - before;
     if (i >= before + w.hi - w.tail) return false;
   } else {
-    const int step = blk / kLpGroups, lane = (blk % kLpGroups) * kLpLanes + (i / kV) % kLpLanes;
-    const int vec = step * kLpStep + i / (kV * kLpLanes) * kLpThreads + lane;
+    const int step = blk / S::kColumns, lane = (blk % S::kColumns) * S::kLanes + (i / kV) % S::kLanes;
+    const int vec = step * S::kStep + i / (kV * S::kLanes) * S::kThreads + lane;
     if (vec >= w.vecs) return false;
     id = w.first + vec * kV + i % kV;
   }
@@ -183,10 +202,10 @@ __device__ __forceinline__ bool lp_element(const T* row, const LpPart& w, int bl
 }
 
 // Lists what the blocks in L.blocks hold above the bound (or at it, with_ties), a vector a thread at a time; stops once the list is past
-// its size.  Returns how many there are, kLpList + 1 if too many.
-template <typename T>
-__device__ __forceinline__ int lp_gather(const T* row, const LpPart& w, unsigned bound, bool with_ties, LpLds& L) {
-  constexpr int kV = LpType<T>::kV, kPer = kLpLanes * kLpVecs;
+// its size.  Returns how many there are, S::kList + 1 if too many.
+template <typename S, typename T>
+__device__ __forceinline__ int lp_gather(const T* row, const LpPart& w, unsigned bound, bool with_ties, LpLds<S>& L) {
+  constexpr int kV = LpType<T>::kV, kPer = S::kLanes * kLpVecs;
   __syncthreads();
   if (threadIdx.x == 0) L.n_list = 0;
   __syncthreads();
@@ -194,118 +213,124 @@ __device__ __forceinline__ int lp_gather(const T* row, const LpPart& w, unsigned
     const unsigned o = lp_order(z);
     if (o > bound || (with_ties && o == bound)) {
       const int at = atomicAdd(&L.n_list, 1);
-      if (at < kLpList) L.list[at] = lp_key(z, id);
+      if (at < S::kList) L.list[at] = lp_key(z, id);
     }
   };
+  if (L.n_blocks > S::kList) return S::kList + 1;
   const int all = L.n_blocks * kPer;
-  for (int i = threadIdx.x; i < all; i += kLpThreads) {
-    if (*(volatile int*)&L.n_list > kLpList) break;
-    const int blk = L.blocks[i / kPer], u = i % kPer;
-    if (blk == kLpBlocks) {  // outside whole vectors: less than a vector's elements before, and after them
-      int id;
-      float z;
-      if (u < 2 * kV && lp_element(row, w, blk, u, id, z)) offer(z, id);
-      continue;
-    }
-    const int vec = blk / kLpGroups * kLpStep + u / kLpLanes * kLpThreads + blk % kLpGroups * kLpLanes + u % kLpLanes;
-    if (vec >= w.vecs) continue;
-    const int id = w.first + vec * kV;
-    float x[kV];
-    lp_widen<T>(*(const u32x4_t*)(row + id), x);
+  constexpr int kBatch = 4;  // loads of a thread on their way together
+  for (int i0 = threadIdx.x; i0 < all; i0 += kBatch * S::kThreads) {
+    if (*(volatile int*)&L.n_list > S::kList) break;
+    u32x4_t raw[kBatch];
+    int ids[kBatch];
 #pragma unroll
-    for (int e = 0; e < kV; ++e) offer(x[e], id + e);
+    for (int k = 0; k < kBatch; ++k) {
+      const int i = i0 + k * S::kThreads;
+      ids[k] = -1;
+      if (i >= all) continue;
+      const int blk = L.blocks[i / kPer], u = i % kPer;
+      if (blk == S::kBlocks) {  // outside whole vectors: less than a vector's elements before, and after them
+        for (int e = u; e < 2 * kV; e += kPer) {
+          int id;
+          float z;
+          if (lp_element<S>(row, w, blk, e, id, z)) offer(z, id);
+        }
+        continue;
+      }
+      const int vec = blk / S::kColumns * S::kStep + u / S::kLanes * S::kThreads + blk % S::kColumns * S::kLanes + u % S::kLanes;
+      if (vec >= w.vecs) continue;
+      ids[k] = w.first + vec * kV;
+      raw[k] = *(const u32x4_t*)(row + ids[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (ids[k] < 0) continue;
+      float x[kV];
+      lp_widen<T>(raw[k], x);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) offer(x[e], ids[k] + e);
+    }
   }
   __syncthreads();
-  return min(L.n_list, kLpList + 1);
+  return min(L.n_list, S::kList + 1);
 }
 
 // lists the blocks whose maximum reaches the bound (above: is above it)
-__device__ __forceinline__ void lp_blocks(int steps, unsigned bound, bool above, LpLds& L) {
+template <typename S>
+__device__ __forceinline__ void lp_blocks(int steps, unsigned bound, bool above, LpLds<S>& L) {
   __syncthreads();
   if (threadIdx.x == 0) L.n_blocks = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i <= steps * kLpGroups; i += kLpThreads) {
-    const int blk = i < steps * kLpGroups ? i : kLpBlocks;
+  for (int i = threadIdx.x; i <= steps * S::kColumns; i += S::kThreads) {
+    const int blk = i < steps * S::kColumns ? i : S::kBlocks;
     const unsigned o = lp_order(L.bm[blk]);
-    if (above ? o > bound : o >= bound) L.blocks[atomicAdd(&L.n_blocks, 1)] = (unsigned short)blk;
+    if (above ? o > bound : o >= bound) {
+      const int at = atomicAdd(&L.n_blocks, 1);
+      if (at < S::kList) L.blocks[at] = (unsigned short)blk;
+    }
   }
   __syncthreads();
 }
 
 // The n largest of the part, by value and then by id, to out(rank, key): every rank below n is given, key 0 where there is none.
-template <typename T, typename Out>
-__device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int n, LpLds& L, Out out) {
-  constexpr int kV = LpType<T>::kV, kBlock = kV * kLpLanes * kLpVecs;
+template <typename S, typename T, typename Out>
+__device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int steps, int n, LpLds<S>& L, Out out) {
+  constexpr int kV = LpType<T>::kV, kBlock = kV * S::kLanes * kLpVecs;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // The n-th largest column maximum: as good a bound for most rows, and one wavefront finds it by counting, without a barrier.
   unsigned bound;
   {
-    static_assert(kLpGroups <= kWave && kLpGroups >= kLpMaxTop, "a column a lane");
-    const unsigned mine = lane < kLpGroups ? lp_order(L.col[lane]) : 0u;
+    static_assert(S::kColumns == kWave && S::kColumns >= kLpMaxTop, "a column a lane");
+    const unsigned mine = (lp_order(L.col[lane]) & ~63u) | lane;  // (distinct; a bound may be lower)
     int above = 0;
 #pragma unroll
-    for (int i = 0; i < kLpGroups; ++i) {
-      const unsigned other = __builtin_amdgcn_readlane(mine, i);
-      above += other > mine || (other == mine && i < lane);
-    }
-    bound = __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)__ballot(above == n - 1)) - 1);
+    for (int i = 0; i < S::kColumns; ++i) above += (unsigned)__builtin_amdgcn_readlane(mine, i) > mine;
+    bound = __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)__ballot(above == n - 1)) - 1) & ~63u;
   }
-  lp_blocks(w.steps, bound, false, L);
-  int count = lp_gather(row, w, bound, true, L);
+  lp_blocks<S>(steps, bound, false, L);
+  int count = lp_gather<S>(row, w, bound, true, L);
   bool ties = false;  // the equal ones are still to be found
-  if (count > kLpList) {
+  if (count > S::kList) {
     // The n-th largest block maximum is closer, and less than n blocks are above it.
-    const int used = w.steps * kLpGroups;
-    {
-      constexpr int kPer = (kLpBlocks + kLpThreads - 1) / kLpThreads;
-      unsigned v[kPer + 1];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = tid + i * kLpThreads < used ? lp_order(L.bm[tid + i * kLpThreads]) : 0u;
-      v[kPer] = tid == 0 ? lp_order(L.bm[kLpBlocks]) : 0u;
-      bound = lp_nth(v, n, L);
-    }
-    lp_blocks(w.steps, bound, true, L);
-    count = lp_gather(row, w, bound, false, L);
+    const int used = steps * S::kColumns;
+    bound = lp_nth<S>(used + 1, n, L, [&](int i) { return lp_order(L.bm[i < used ? i : S::kBlocks]); });
+    lp_blocks<S>(steps, bound, true, L);
+    count = lp_gather<S>(row, w, bound, false, L);
     ties = true;
-    if (count > kLpList) {
+    if (count > S::kList) {
       // They hold more than the list: the n-th largest element is among theirs.
-      constexpr int kPer = (kLpMaxTop * kBlock + kLpThreads - 1) / kLpThreads;
-      unsigned v[kPer];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int e = tid + i * kLpThreads;
+      bound = lp_nth<S>(L.n_blocks * kBlock, n, L, [&](int i) {
         int id;
         float z;
-        v[i] = e < L.n_blocks * kBlock && lp_element(row, w, L.blocks[e / kBlock], e % kBlock, id, z) ? lp_order(z) : 0u;
-      }
-      bound = lp_nth(v, n, L);
-      count = lp_gather(row, w, bound, true, L);
-      ties = count > kLpList;
-      if (ties) count = lp_gather(row, w, bound, false, L);
+        return lp_element<S>(row, w, L.blocks[i / kBlock], i % kBlock, id, z) ? lp_order(z) : 0u;
+      });
+      count = lp_gather<S>(row, w, bound, true, L);
+      ties = count > S::kList;
+      if (ties) count = lp_gather<S>(row, w, bound, false, L);
     }
   }
-  // rank by counting
-  for (int i = tid; i < count; i += kLpThreads) {
+  if (tid < kLpRankStep) L.list[count + tid] = 0;
+  __syncthreads();
+  for (int i = tid; i < count; i += S::kThreads) {
     const unsigned long long k = L.list[i];
-    int rank = 0;
-    for (int j = 0; j < count; ++j) rank += L.list[j] > k;
+    const int rank = lp_rank(L.list, count, k);
     if (rank < n) out(rank, k);
   }
   int have = min(count, n);
   if (ties && have < n) {
     // Equal values in the order of their ids: the row's pieces in order, in each the lowest id not yet taken.
     const float at = lp_value(bound);
-    for (int piece = -1; piece <= w.steps && have < n; ++piece) {
+    for (int piece = -1; piece <= steps && have < n; ++piece) {
       int ids[kLpVecs * kV];
       int m = 0;
-      if (piece < 0 || piece == w.steps) {  // the elements before, and after, the vectors
+      if (piece < 0 || piece == steps) {  // the elements before, and after, the vectors
         const int id = (piece < 0 ? w.lo : w.tail) + tid;
         ids[0] = id < (piece < 0 ? w.first : w.hi) && to_f32<T>(row[id]) == at ? id : INT32_MAX;
         m = 1;
       } else {
 #pragma unroll
         for (int u = 0; u < kLpVecs; ++u) {
-          const int vec = piece * kLpStep + u * kLpThreads + tid;
+          const int vec = piece * S::kStep + u * S::kThreads + tid;
 #pragma unroll
           for (int e = 0; e < kV; ++e) {
             const int id = w.first + vec * kV + e;
@@ -325,7 +350,7 @@ __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int n, 
         if (lane == 0) L.best[wave] = low;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kLpWaves; ++i) low = min(low, L.best[i]);
+        for (int i = 0; i < S::kWaves; ++i) low = min(low, L.best[i]);
         if (low == INT32_MAX) break;
         if (tid == 0) out(have, lp_key(at, low));
         ++have;
@@ -333,17 +358,17 @@ __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int n, 
       }
     }
   }
-  for (int i = have + tid; i < n; i += kLpThreads) out(i, 0ull);
+  for (int i = have + tid; i < n; i += S::kThreads) out(i, 0ull);
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------------------
-template <typename T, bool kTop>
-__global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch P) {
+template <typename T, typename S, bool kTop>
+__global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch P) {
   constexpr int kV = LpType<T>::kV;
-  __shared__ LpSums s_part[kLpWaves];
-  __shared__ float s_m[kLpWaves];
+  __shared__ LpSums s_part[S::kWaves];
+  __shared__ float s_m[S::kWaves];
   __shared__ double s_lse2;
-  __shared__ typename std::conditional<kTop, LpLds, int>::type s_lds;
+  __shared__ typename std::conditional<kTop, LpLds<S>, int>::type s_lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const long long task = (long long)blockIdx.y * kLpGridRows + blockIdx.x;
   if (task >= (long long)P.rows * P.splits) return;  // the whole workgroup
@@ -351,14 +376,15 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch 
   const int split = (int)(task - (long long)row * P.splits);
   const T* z = (const T*)P.logits + row * (size_t)P.row_stride;
   const LpPart w = lp_part(z, P.V, split, P.splits);
+  const int steps = (w.vecs + S::kStep - 1) / S::kStep;
   const u32x4_t* vp = (const u32x4_t*)(z + w.first);
 
   u32x4_t cur[kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
 #pragma unroll
-    for (int u = 0; u < kLpVecs; ++u) v[u] = __builtin_nontemporal_load(vp + min(step * kLpStep + u * kLpThreads + tid, w.vecs - 1));
+    for (int u = 0; u < kLpVecs; ++u) v[u] = __builtin_nontemporal_load(vp + min(step * S::kStep + u * S::kThreads + tid, w.vecs - 1));
   };
-  if (w.steps > 0) load(0, cur);
+  if (steps > 0) load(0, cur);
   const float c = lp_scale(P, row);
   const int token = P.tokens ? P.tokens[row] : -1;
   const bool known = token >= 0 && token < P.V;
@@ -401,26 +427,27 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch 
     for (int u = 0; u < kLpVecs; ++u) {
       float y[kV];
       lp_widen<T>(cur[u], y);
-      const bool in = kWhole || step * kLpStep + u * kLpThreads + tid < w.vecs;
+      const bool in = kWhole || step * S::kStep + u * S::kThreads + tid < w.vecs;
 #pragma unroll
       for (int e = 0; e < kV; ++e) x[u * kV + e] = in ? y[e] : -INFINITY;
     }
-    if (step + 1 < w.steps) load(step + 1, cur);
+    if (step + 1 < steps) load(step + 1, cur);
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kLpVecs * kV; i += 2) top = fmaxf(fmaxf(x[i], x[i + 1]), top);
     add(x, top);
     if constexpr (kTop) {
-      // over the block's eight lanes: neighbours, pairs, then the other four
-      top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0xB1, 0xf, 0xf, true)));
-      top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x4E, 0xf, 0xf, true)));
-      top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x141, 0xf, 0xf, true)));
-      if (tid % kLpLanes == 0) s_lds.bm[step * kLpGroups + tid / kLpLanes] = top;
+      if constexpr (S::kLanes > 1) {  // over the block's four lanes: neighbours, then pairs
+        static_assert(S::kLanes == 4 || S::kLanes == 1, "");
+        top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0xB1, 0xf, 0xf, true)));
+        top = fmaxf(top, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(top), 0x4E, 0xf, 0xf, true)));
+      }
+      if (tid % S::kLanes == 0) s_lds.bm[step * S::kColumns + tid / S::kLanes] = top;
       col = fmaxf(col, top);
     }
   };
-  for (int step = 0; step < w.steps; ++step) {
-    if ((step + 1) * kLpStep <= w.vecs) take(step, std::true_type{});
+  for (int step = 0; step < steps; ++step) {
+    if ((step + 1) * S::kStep <= w.vecs) take(step, std::true_type{});
     else take(step, std::false_type{});
   }
   {  // the elements outside whole vectors: one each for the first threads
@@ -435,9 +462,9 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch 
     if constexpr (kTop) {
       if (wave == 0) {
         top = wave_max(top);
-        if (lane == 0) s_lds.bm[kLpBlocks] = top;
+        if (lane == 0) s_lds.bm[S::kBlocks] = top;
       }
-      if (tid % kLpLanes == 0) s_lds.col[tid / kLpLanes] = col;
+      if (tid % S::kLanes == 0) s_lds.col[tid / S::kLanes] = col;
     }
   }
 
@@ -447,7 +474,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch 
     if (lane == 0) s_m[wave] = m;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kLpWaves; ++i) m = fmaxf(m, s_m[i]);
+    for (int i = 0; i < S::kWaves; ++i) m = fmaxf(m, s_m[i]);
     mine = lp_moved(mine, m, c);
     const double s = wave_sum(mine.s), t = wave_sum(mine.t);
     if (lane == 0) s_part[wave] = {m, s, t};
@@ -456,19 +483,19 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch 
   if (tid == 0) {
     LpSums all = s_part[0];
 #pragma unroll
-    for (int i = 1; i < kLpWaves; ++i) {
+    for (int i = 1; i < S::kWaves; ++i) {
       all.s += s_part[i].s;
       all.t += s_part[i].t;
     }
     if (P.splits == 1) s_lse2 = lp_finish(P, row, all, c, z_t, known);
-    else P.parts[task] = LogprobPart{all.s, all.t, all.m, 0.f};
+    else P.parts[task] = LogprobPart{all.s, all.t, all.m, z_t};
   }
   if constexpr (kTop) {
     if (P.splits > 1) {
       unsigned long long* keys = P.keys + (size_t)task * P.n_top;
-      lp_select(z, w, P.n_top, s_lds, [&](int rank, unsigned long long k) { keys[rank] = k; });
+      lp_select<S>(z, w, steps, P.n_top, s_lds, [&](int rank, unsigned long long k) { keys[rank] = k; });
     } else {
-      lp_select(z, w, P.n_top, s_lds, [&](int rank, unsigned long long k) {
+      lp_select<S>(z, w, steps, P.n_top, s_lds, [&](int rank, unsigned long long k) {
         const double base = s_lse2;  // (the selection has barriers of its own)
         const float v = lp_value((unsigned)(k >> 32));
         const size_t at = row * P.n_top + rank;
@@ -480,60 +507,78 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(LogprobLaunch 
 }
 
 // Joins the parts of a row, one workgroup each.  The parts' lists are sorted, so with more parts than alternatives the n-th largest
-// of their heads is a bound again, and few of their keys reach it.
+// of their heads is a bound again, and few of their keys reach it.  Bound by latency: everything is loaded at once, and one wavefront
+// joins the sums while another looks for the bound.
 constexpr int kLpMergeThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobLaunch P) {
-  __shared__ unsigned long long s_key[kLpMaxSplits * kLpMaxTop];
+  constexpr int kHeld = 2;  // keys of a thread that are loaded ahead
+  __shared__ unsigned long long s_key[kLpMaxSplits * kLpMaxTop + kLpRankStep];
   __shared__ double s_lse2;
   __shared__ int s_n;
   __shared__ unsigned long long s_bound;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const long long at = (long long)blockIdx.y * kLpGridRows + blockIdx.x;
   if (at >= P.rows) return;
   const size_t row = (size_t)at;
+  const int n = P.n_top, parts = P.splits, all = parts * n;
+  const unsigned long long* keys = P.keys + row * all;
+  unsigned long long held[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) held[i] = tid + i * kLpMergeThreads < all ? keys[tid + i * kLpMergeThreads] : 0ull;
   const float c = lp_scale(P, row);
-  const int n = P.n_top, parts = P.splits;
-  if (tid < kWave) {
+  if (wave == 0) {
     LpSums x = {-INFINITY, 0.0, 0.0};
-    if (tid < parts) {
-      const LogprobPart p = P.parts[row * parts + tid];
-      x = {p.m, p.s, p.t};
-    }
+    const int token = P.tokens ? P.tokens[row] : -1;
+    const LogprobPart p = P.parts[row * parts + min(lane, parts - 1)];
+    if (lane < parts) x = {p.m, p.s, p.t};
     const float m = wave_max(x.m);
     x = lp_moved(x, m, c);
     const double s = wave_sum(x.s), t = wave_sum(x.t);
-    if (n > 0) {
-      const unsigned long long head = tid < parts ? P.keys[(row * parts + tid) * n] : 0ull;
+    if (lane == 0) s_lse2 = lp_finish(P, row, {m, s, t}, c, p.z_t, token >= 0 && token < P.V);
+  } else if (wave == 1 && n > 0) {
+    // A bound that n keys reach: the n-th largest head of as many parts, or the smallest of all parts' q-th keys, n of them together.
+    const int q = (n + parts - 1) / parts;
+    const unsigned long long mine = lane < parts ? keys[lane * n + (q - 1)] : ~0ull;
+    unsigned long long bound = 0;
+    if (q > 1) {
+      bound = mine;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const unsigned long long other = __shfl_xor(bound, o, kWave);
+        bound = other < bound ? other : bound;
+      }
+    } else {
+      const unsigned long long head = lane < parts ? mine : 0ull;
       int above = 0;
       for (int i = 0; i < parts; ++i) {
         const unsigned long long other = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(head >> 32), i) << 32 |
                                          (unsigned)__builtin_amdgcn_readlane((int)head, i);
         above += other > head;
       }
-      if (tid == 0) { s_n = 0; s_bound = 0; }
-      if (above == n - 1 && head) s_bound = head;  // (keys are distinct)
+      const unsigned long long nth = __ballot(above == n - 1 && head != 0);  // (keys are distinct)
+      if (nth) bound = __shfl(head, __ffsll(nth) - 1, kWave);
     }
-    if (tid == 0) {
-      const int token = P.tokens ? P.tokens[row] : -1;
-      const bool known = token >= 0 && token < P.V;
-      const float z_t = known ? to_f32<T>(((const T*)P.logits)[row * (size_t)P.row_stride + token]) : 0.f;
-      s_lse2 = lp_finish(P, row, {m, s, t}, c, z_t, known);
-    }
+    if (lane == 0) { s_n = 0; s_bound = bound; }
   }
   if (n == 0) return;
   __syncthreads();
-  for (int i = tid; i < parts * n; i += kLpMergeThreads) {
-    const unsigned long long k = P.keys[row * parts * n + i];
-    if (k && k >= s_bound) s_key[atomicAdd(&s_n, 1)] = k;
+  const unsigned long long bound = s_bound;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (held[i] && held[i] >= bound) s_key[atomicAdd(&s_n, 1)] = held[i];
+  for (int i = tid + kHeld * kLpMergeThreads; i < all; i += kLpMergeThreads) {
+    const unsigned long long k = keys[i];
+    if (k && k >= bound) s_key[atomicAdd(&s_n, 1)] = k;
   }
   __syncthreads();
   const int count = s_n;
   const double base = s_lse2;
+  if (tid < kLpRankStep) s_key[count + tid] = 0;
+  __syncthreads();
   for (int i = tid; i < count; i += kLpMergeThreads) {
     const unsigned long long k = s_key[i];
-    int rank = 0;
-    for (int j = 0; j < count; ++j) rank += s_key[j] > k;
+    const int rank = lp_rank(s_key, count, k);
     if (rank < n) {
       const float v = lp_value((unsigned)(k >> 32));
       P.top_ids[row * n + rank] = (int32_t)(0xffffffffu - (unsigned)k);
@@ -625,25 +670,38 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
 // Workgroups per row: one where the rows fill the chip (256 compute units, several workgroups each), else as many as do, of no less than
 // two steps; and never more than a workgroup's block maxima allow.
 int logprob_splits(int64_t rows, int V, bool bf16) {
-  const int per_vec = bf16 ? 8 : 4;
-  const int64_t vecs = V / per_vec;
-  const int64_t least = (vecs + (int64_t)kLpStep * kLpMaxSteps - 1) / ((int64_t)kLpStep * kLpMaxSteps);
+  constexpr int64_t most = (int64_t)LpWide::kStep * LpWide::kMaxSteps;
+  const int64_t vecs = V / (bf16 ? 8 : 4), least = (vecs + most - 1) / most;
   int64_t want = rows >= 1024 ? 1 : (1279 + rows) / std::max<int64_t>(rows, 1);
-  want = std::min<int64_t>(want, vecs / (2 * kLpStep));
+  want = std::min<int64_t>(want, vecs / (2 * LpWide::kStep));
   want = std::min<int64_t>(want, kLpMaxSplits);
   return (int)std::max<int64_t>(std::max<int64_t>(want, least), 1);
 }
 int logprob_max_top() { return kLpMaxTop; }
-int logprob_max_vocab() { return kLpMaxSplits * kLpMaxSteps * kLpStep * 4; }
+int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kStep * 4; }
 
+// Rows of so few vectors go to a wavefront each where there are many: what a row costs besides its bytes is barriers, the more of them with
+// a selection.  us with 256 threads a row and with 64: 60000 rows x 777 fp32 136 and 51, with one alternative 399 and 117; 20000 x 2048 53
+// and 31, with five 141 and 52; 10000 x 16001 bf16 with five 114 and 75; 10000 x 8192 fp32 without 53 and 55.
+constexpr int kLpNarrowVecs = 1024, kLpNarrowVecsTop = 4096, kLpNarrowRows = 1024;
+static_assert(kLpNarrowVecsTop <= LpNarrow::kStep * LpNarrow::kMaxSteps, "a row's block maxima");
+
+static dim3 logprob_grid(int64_t n) {
+  return dim3((unsigned)std::min<int64_t>(n, kLpGridRows), (unsigned)((n + kLpGridRows - 1) / kLpGridRows));
+}
 template <typename T>
 static hipError_t launch_logprob_t(const LogprobLaunch& P, hipStream_t st) {
-  const int64_t tasks = (int64_t)P.rows * P.splits;
-  auto grid = [](int64_t n) { return dim3((unsigned)std::min<int64_t>(n, kLpGridRows), (unsigned)((n + kLpGridRows - 1) / kLpGridRows)); };
-  if (P.n_top > 0) hipLaunchKernelGGL((logprob_rows_kernel<T, true>), grid(tasks), dim3(kLpThreads), 0, st, P);
-  else hipLaunchKernelGGL((logprob_rows_kernel<T, false>), grid(tasks), dim3(kLpThreads), 0, st, P);
+  const dim3 grid = logprob_grid((int64_t)P.rows * P.splits);
+#define AURORA_LOGPROB(S)                                                                                             \
+  do {                                                                                                                \
+    if (P.n_top > 0) hipLaunchKernelGGL((logprob_rows_kernel<T, S, true>), grid, dim3(S::kThreads), 0, st, P);        \
+    else hipLaunchKernelGGL((logprob_rows_kernel<T, S, false>), grid, dim3(S::kThreads), 0, st, P);                   \
+  } while (0)
+  if (P.splits == 1 && P.rows >= kLpNarrowRows && P.V / LpType<T>::kV <= (P.n_top > 0 ? kLpNarrowVecsTop : kLpNarrowVecs)) AURORA_LOGPROB(LpNarrow);
+  else AURORA_LOGPROB(LpWide);
+#undef AURORA_LOGPROB
   if (hipError_t e = hipGetLastError(); e != hipSuccess || P.splits == 1) return e;
-  hipLaunchKernelGGL(logprob_merge_kernel<T>, grid(P.rows), dim3(kLpMergeThreads), 0, st, P);
+  hipLaunchKernelGGL(logprob_merge_kernel<T>, logprob_grid(P.rows), dim3(kLpMergeThreads), 0, st, P);
   return hipGetLastError();
 }
 hipError_t launch_logprob(const LogprobLaunch& P, hipStream_t st) {
@@ -656,8 +714,7 @@ hipError_t launch_logprob_backward(const LogprobLaunch& P0, hipStream_t st) {
   // a workgroup takes about four rounds of its loads
   P.wide = (((uintptr_t)P.grad ^ (uintptr_t)P.logits) & 15) == 0;
   P.splits = (int)std::max<int64_t>(1, std::min<int64_t>((vecs + 4095) / 4096, 4096));
-  const int64_t tasks = (int64_t)P.rows * P.splits;
-  const dim3 grid((unsigned)std::min<int64_t>(tasks, kLpGridRows), (unsigned)((tasks + kLpGridRows - 1) / kLpGridRows));
+  const dim3 grid = logprob_grid((int64_t)P.rows * P.splits);
   if (P.bf16) hipLaunchKernelGGL(logprob_backward_kernel<bf16_t>, grid, dim3(kLpBackThreads), 0, st, P);
   else hipLaunchKernelGGL(logprob_backward_kernel<float>, grid, dim3(kLpBackThreads), 0, st, P);
   return hipGetLastError();
