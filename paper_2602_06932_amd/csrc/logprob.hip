@@ -96,6 +96,39 @@ constexpr float kLpFar = 8.5e37f;
 __device__ __forceinline__ bool lp_far(float m, float c) { return fabsf(m) * c > kLpFar; }
 __device__ __forceinline__ double lp_ref(float m, float c) { return lp_far(m, c) ? (double)m * (double)c : (double)(m * c); }
 
+// reductions over a wavefront by data-parallel moves: within rows of sixteen, then across; every lane gets the result
+template <int kCtl, int kRows>
+__device__ __forceinline__ float lp_max_step(float v) {
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp((int)0xff800000u, __float_as_int(v), kCtl, kRows, 0xf, false)));
+}
+__device__ __forceinline__ float lp_wave_max(float v) {
+  v = lp_max_step<0x111, 0xf>(v);
+  v = lp_max_step<0x112, 0xf>(v);
+  v = lp_max_step<0x114, 0xf>(v);
+  v = lp_max_step<0x118, 0xf>(v);
+  v = lp_max_step<0x142, 0xa>(v);
+  v = lp_max_step<0x143, 0xc>(v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+template <int kCtl, int kRows>
+__device__ __forceinline__ double lp_sum_step(double v) {
+  const long long b = __double_as_longlong(v);
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)b, kCtl, kRows, 0xf, false);
+  const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), kCtl, kRows, 0xf, false);
+  return v + __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+__device__ __forceinline__ double lp_wave_sum(double v) {
+  v = lp_sum_step<0x111, 0xf>(v);
+  v = lp_sum_step<0x112, 0xf>(v);
+  v = lp_sum_step<0x114, 0xf>(v);
+  v = lp_sum_step<0x118, 0xf>(v);
+  v = lp_sum_step<0x142, 0xa>(v);
+  v = lp_sum_step<0x143, 0xc>(v);
+  const long long b = __double_as_longlong(v);
+  return __longlong_as_double((long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(b >> 32), 63) << 32 |
+                                          (unsigned)__builtin_amdgcn_readlane((int)b, 63)));
+}
+
 struct LpSums { float m; double s, t; };
 // the sums with reference `to` (the largest of several, c as above); nothing so far counts for nothing
 __device__ __forceinline__ LpSums lp_moved(const LpSums& a, float to, float c) {
@@ -272,23 +305,24 @@ __device__ __forceinline__ void lp_blocks(int steps, unsigned bound, bool above,
   __syncthreads();
 }
 
-// The n largest of the part, by value and then by id, to out(rank, key): every rank below n is given, key 0 where there is none.
+// The n-th largest column maximum, or a little less: as good a bound for most rows, and a wavefront finds it by counting, without a barrier.
+template <typename S>
+__device__ __forceinline__ unsigned lp_column_bound(int n, const LpLds<S>& L) {
+  static_assert(S::kColumns == kWave && S::kColumns >= kLpMaxTop, "a column a lane");
+  const int lane = threadIdx.x & 63;
+  const unsigned mine = (lp_order(L.col[lane]) & ~63u) | lane;  // (distinct)
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < S::kColumns; ++i) above += (unsigned)__builtin_amdgcn_readlane(mine, i) > mine;
+  return __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)__ballot(above == n - 1)) - 1) & ~63u;
+}
+
+// The n largest of the part, by value and then by id, to out(rank, key): every rank below n is given, key 0 where there is none.  The list
+// holds the `count` elements that reach the bound (past its size: more than it takes).
 template <typename S, typename T, typename Out>
-__device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int steps, int n, LpLds<S>& L, Out out) {
+__device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int steps, int n, unsigned bound, int count, LpLds<S>& L, Out out) {
   constexpr int kV = LpType<T>::kV, kBlock = kV * S::kLanes * kLpVecs;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // The n-th largest column maximum: as good a bound for most rows, and one wavefront finds it by counting, without a barrier.
-  unsigned bound;
-  {
-    static_assert(S::kColumns == kWave && S::kColumns >= kLpMaxTop, "a column a lane");
-    const unsigned mine = (lp_order(L.col[lane]) & ~63u) | lane;  // (distinct; a bound may be lower)
-    int above = 0;
-#pragma unroll
-    for (int i = 0; i < S::kColumns; ++i) above += (unsigned)__builtin_amdgcn_readlane(mine, i) > mine;
-    bound = __builtin_amdgcn_readlane(mine, __ffsll((unsigned long long)__ballot(above == n - 1)) - 1) & ~63u;
-  }
-  lp_blocks<S>(steps, bound, false, L);
-  int count = lp_gather<S>(row, w, bound, true, L);
   bool ties = false;  // the equal ones are still to be found
   if (count > S::kList) {
     // The n-th largest block maximum is closer, and less than n blocks are above it.
@@ -362,7 +396,9 @@ __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int ste
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------------------
-template <typename T, typename S, bool kTop>
+// kHeld: the part is at most so many steps long (P.splits sees to that): all of it is on its way at once and stays in registers, so
+// that a selection reads nothing again.  0: a step at a time, the next one on its way.
+template <typename T, typename S, bool kTop, int kHeld>
 __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch P) {
   constexpr int kV = LpType<T>::kV;
   __shared__ LpSums s_part[S::kWaves];
@@ -370,21 +406,27 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   __shared__ double s_lse2;
   __shared__ typename std::conditional<kTop, LpLds<S>, int>::type s_lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const long long task = (long long)blockIdx.y * kLpGridRows + blockIdx.x;
-  if (task >= (long long)P.rows * P.splits) return;  // the whole workgroup
-  const size_t row = (size_t)(task / P.splits);
-  const int split = (int)(task - (long long)row * P.splits);
+  const unsigned task = blockIdx.y * (unsigned)kLpGridRows + blockIdx.x;
+  if (task >= (unsigned)P.rows * (unsigned)P.splits) return;  // the whole workgroup
+  const size_t row = task / (unsigned)P.splits;
+  const int split = task % (unsigned)P.splits;
   const T* z = (const T*)P.logits + row * (size_t)P.row_stride;
   const LpPart w = lp_part(z, P.V, split, P.splits);
   const int steps = (w.vecs + S::kStep - 1) / S::kStep;
   const u32x4_t* vp = (const u32x4_t*)(z + w.first);
 
-  u32x4_t cur[kLpVecs];
+  u32x4_t cur[kHeld > 0 ? kHeld : 1][kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
 #pragma unroll
     for (int u = 0; u < kLpVecs; ++u) v[u] = __builtin_nontemporal_load(vp + min(step * S::kStep + u * S::kThreads + tid, w.vecs - 1));
   };
-  if (steps > 0) load(0, cur);
+  if constexpr (kHeld > 0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (i < steps) load(i, cur[i]);
+  } else {
+    if (steps > 0) load(0, cur[0]);
+  }
   const float c = lp_scale(P, row);
   const int token = P.tokens ? P.tokens[row] : -1;
   const bool known = token >= 0 && token < P.V;
@@ -420,21 +462,23 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   };
 
   // one step's elements, the next step's already on their way; kWhole: no vector of the step lies past the part
-  auto take = [&](int step, auto whole) {
+  float tops[kHeld > 0 ? kHeld : 1];  // a held step's maximum
+  auto take = [&](int step, u32x4_t (&v)[kLpVecs], float& held_top, auto whole) {
     constexpr bool kWhole = decltype(whole)::value;
     float x[kLpVecs * kV];
 #pragma unroll
     for (int u = 0; u < kLpVecs; ++u) {
       float y[kV];
-      lp_widen<T>(cur[u], y);
+      lp_widen<T>(v[u], y);
       const bool in = kWhole || step * S::kStep + u * S::kThreads + tid < w.vecs;
 #pragma unroll
       for (int e = 0; e < kV; ++e) x[u * kV + e] = in ? y[e] : -INFINITY;
     }
-    if (step + 1 < steps) load(step + 1, cur);
+    if (kHeld == 0 && step + 1 < steps) load(step + 1, v);
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kLpVecs * kV; i += 2) top = fmaxf(fmaxf(x[i], x[i + 1]), top);
+    held_top = top;
     add(x, top);
     if constexpr (kTop) {
       if constexpr (S::kLanes > 1) {  // over the block's four lanes: neighbours, then pairs
@@ -446,41 +490,55 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
       col = fmaxf(col, top);
     }
   };
-  for (int step = 0; step < steps; ++step) {
-    if ((step + 1) * S::kStep <= w.vecs) take(step, std::true_type{});
-    else take(step, std::false_type{});
+  if constexpr (kHeld > 0) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      tops[i] = -INFINITY;
+      if (i >= steps) continue;
+      if ((i + 1) * S::kStep <= w.vecs) take(i, cur[i], tops[i], std::true_type{});
+      else take(i, cur[i], tops[i], std::false_type{});
+    }
+  } else {
+    for (int step = 0; step < steps; ++step) {
+      if ((step + 1) * S::kStep <= w.vecs) take(step, cur[0], tops[0], std::true_type{});
+      else take(step, cur[0], tops[0], std::false_type{});
+    }
   }
+  int edge;
+  float edge_z = 0.f;
   {  // the elements outside whole vectors: one each for the first threads
     const int before = w.first - w.lo, edges = before + w.hi - w.tail;
     float x[1] = {-INFINITY};
     float top = -INFINITY;
-    if (tid < edges) {
-      x[0] = to_f32<T>(z[tid < before ? w.lo + tid : w.tail + tid - before]);
+    edge = tid < edges ? (tid < before ? w.lo + tid : w.tail + tid - before) : -1;
+    if (edge >= 0) {
+      x[0] = edge_z = to_f32<T>(z[edge]);
       top = fmaxf(x[0], -INFINITY);  // (not a NaN)
       add(x, top);
     }
     if constexpr (kTop) {
       if (wave == 0) {
-        top = wave_max(top);
+        top = lp_wave_max(top);
         if (lane == 0) s_lds.bm[S::kBlocks] = top;
       }
       if (tid % S::kLanes == 0) s_lds.col[tid / S::kLanes] = col;
+      if (tid == 0) s_lds.n_list = 0;
     }
   }
 
   // ---- the workgroup's sums ------------------------------------------------------------------------------------
   {
-    float m = wave_max(mine.m);
+    float m = lp_wave_max(mine.m);
     if (lane == 0) s_m[wave] = m;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < S::kWaves; ++i) m = fmaxf(m, s_m[i]);
     mine = lp_moved(mine, m, c);
-    const double s = wave_sum(mine.s), t = wave_sum(mine.t);
+    const double s = lp_wave_sum(mine.s), t = lp_wave_sum(mine.t);
     if (lane == 0) s_part[wave] = {m, s, t};
   }
   __syncthreads();
-  if (tid == 0) {
+  if (tid == S::kThreads - 1) {  // (a lane of the last wavefront: the first has the elements outside vectors)
     LpSums all = s_part[0];
 #pragma unroll
     for (int i = 1; i < S::kWaves; ++i) {
@@ -488,17 +546,52 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
       all.t += s_part[i].t;
     }
     if (P.splits == 1) s_lse2 = lp_finish(P, row, all, c, z_t, known);
-    else P.parts[task] = LogprobPart{all.s, all.t, all.m, z_t};
+    else P.parts[(size_t)task] = LogprobPart{all.s, all.t, all.m, z_t};
   }
   if constexpr (kTop) {
-    if (P.splits > 1) {
-      unsigned long long* keys = P.keys + (size_t)task * P.n_top;
-      lp_select<S>(z, w, steps, P.n_top, s_lds, [&](int rank, unsigned long long k) { keys[rank] = k; });
+    LpLds<S>& L = s_lds;
+    const int n = P.n_top;
+    const unsigned bound = lp_column_bound(n, L);
+    int count;
+    if constexpr (kHeld > 0) {
+      const float at_least = fmaxf(lp_value(bound), -INFINITY);  // (below the key of -inf come NaNs)
+      auto offer = [&](float v, int id) {
+        if (v >= at_least) {
+          const int at = atomicAdd(&L.n_list, 1);
+          if (at < S::kList) L.list[at] = lp_key(v, id);
+        }
+      };
+      if (edge >= 0) offer(edge_z, edge);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) {
+        if (i >= steps || !(tops[i] >= at_least)) continue;
+#pragma unroll
+        for (int u = 0; u < kLpVecs; ++u) {
+          const int vec = i * S::kStep + u * S::kThreads + tid;
+          float y[kV], top = -INFINITY;
+          lp_widen<T>(cur[i][u], y);
+#pragma unroll
+          for (int e = 0; e < kV; e += 2) top = fmaxf(fmaxf(y[e], y[e + 1]), top);
+          if (vec < w.vecs && top >= at_least) {
+#pragma unroll
+            for (int e = 0; e < kV; ++e) offer(y[e], w.first + vec * kV + e);
+          }
+        }
+      }
+      __syncthreads();
+      count = min(L.n_list, S::kList + 1);
     } else {
-      lp_select<S>(z, w, steps, P.n_top, s_lds, [&](int rank, unsigned long long k) {
-        const double base = s_lse2;  // (the selection has barriers of its own)
+      lp_blocks<S>(steps, bound, false, L);
+      count = lp_gather<S>(z, w, bound, true, L);
+    }
+    if (P.splits > 1) {
+      unsigned long long* keys = P.keys + (size_t)task * n;
+      lp_select<S>(z, w, steps, n, bound, count, L, [&](int rank, unsigned long long k) { keys[rank] = k; });
+    } else {
+      lp_select<S>(z, w, steps, n, bound, count, L, [&](int rank, unsigned long long k) {
+        const double base = s_lse2;  // (there are barriers in between)
         const float v = lp_value((unsigned)(k >> 32));
-        const size_t at = row * P.n_top + rank;
+        const size_t at = row * n + rank;
         P.top_ids[at] = k ? (int32_t)(0xffffffffu - (unsigned)k) : -1;
         P.top_logprobs[at] = k && v > -INFINITY ? (float)(kLpLn2 * ((double)v * (double)c - base)) : -INFINITY;
       });
@@ -532,9 +625,9 @@ __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobL
     const int token = P.tokens ? P.tokens[row] : -1;
     const LogprobPart p = P.parts[row * parts + min(lane, parts - 1)];
     if (lane < parts) x = {p.m, p.s, p.t};
-    const float m = wave_max(x.m);
+    const float m = lp_wave_max(x.m);
     x = lp_moved(x, m, c);
-    const double s = wave_sum(x.s), t = wave_sum(x.t);
+    const double s = lp_wave_sum(x.s), t = lp_wave_sum(x.t);
     if (lane == 0) s_lse2 = lp_finish(P, row, {m, s, t}, c, p.z_t, token >= 0 && token < P.V);
   } else if (wave == 1 && n > 0) {
     // A bound that n keys reach: the n-th largest head of as many parts, or the smallest of all parts' q-th keys, n of them together.
@@ -598,10 +691,10 @@ template <typename T>
 __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(LogprobLaunch P) {
   constexpr int kV = LpType<T>::kV;
   const int tid = threadIdx.x;
-  const long long task = (long long)blockIdx.y * kLpGridRows + blockIdx.x;
-  if (task >= (long long)P.rows * P.splits) return;
-  const size_t row = (size_t)(task / P.splits);
-  const int split = (int)(task - (long long)row * P.splits);
+  const unsigned task = blockIdx.y * (unsigned)kLpGridRows + blockIdx.x;
+  if (task >= (unsigned)P.rows * (unsigned)P.splits) return;
+  const size_t row = task / (unsigned)P.splits;
+  const int split = task % (unsigned)P.splits;
   const T* z = (const T*)P.logits + row * (size_t)P.row_stride;
   T* g = (T*)P.grad + row * (size_t)P.row_stride;
   const LpPart w = lp_part(z, P.V, split, P.splits);
@@ -667,15 +760,13 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
-// Workgroups per row: one where the rows fill the chip (256 compute units, several workgroups each), else as many as do, of no less than
-// two steps; and never more than a workgroup's block maxima allow.
+// Workgroups per row: one where the rows fill the chip (256 compute units, several workgroups each); few rows are cut into parts that a
+// workgroup holds in registers.  And never more than a workgroup's block maxima allow.
+constexpr int kLpHeld = 4, kLpFewRows = 640;
 int logprob_splits(int64_t rows, int V, bool bf16) {
-  constexpr int64_t most = (int64_t)LpWide::kStep * LpWide::kMaxSteps;
-  const int64_t vecs = V / (bf16 ? 8 : 4), least = (vecs + most - 1) / most;
-  int64_t want = rows >= 1024 ? 1 : (1279 + rows) / std::max<int64_t>(rows, 1);
-  want = std::min<int64_t>(want, vecs / (2 * LpWide::kStep));
-  want = std::min<int64_t>(want, kLpMaxSplits);
-  return (int)std::max<int64_t>(std::max<int64_t>(want, least), 1);
+  constexpr int64_t most = (int64_t)LpWide::kStep * LpWide::kMaxSteps, held = (int64_t)LpWide::kStep * kLpHeld;
+  const int64_t vecs = V / (bf16 ? 8 : 4), least = (vecs + most - 1) / most, want = (vecs + held - 1) / held;
+  return (int)std::max<int64_t>(rows <= kLpFewRows && want <= kLpMaxSplits ? want : least, 1);
 }
 int logprob_max_top() { return kLpMaxTop; }
 int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kStep * 4; }
@@ -692,13 +783,15 @@ static dim3 logprob_grid(int64_t n) {
 template <typename T>
 static hipError_t launch_logprob_t(const LogprobLaunch& P, hipStream_t st) {
   const dim3 grid = logprob_grid((int64_t)P.rows * P.splits);
-#define AURORA_LOGPROB(S)                                                                                             \
+#define AURORA_LOGPROB(S, HELD)                                                                                        \
   do {                                                                                                                \
-    if (P.n_top > 0) hipLaunchKernelGGL((logprob_rows_kernel<T, S, true>), grid, dim3(S::kThreads), 0, st, P);        \
-    else hipLaunchKernelGGL((logprob_rows_kernel<T, S, false>), grid, dim3(S::kThreads), 0, st, P);                   \
+    if (P.n_top > 0) hipLaunchKernelGGL((logprob_rows_kernel<T, S, true, HELD>), grid, dim3(S::kThreads), 0, st, P);  \
+    else hipLaunchKernelGGL((logprob_rows_kernel<T, S, false, HELD>), grid, dim3(S::kThreads), 0, st, P);             \
   } while (0)
-  if (P.splits == 1 && P.rows >= kLpNarrowRows && P.V / LpType<T>::kV <= (P.n_top > 0 ? kLpNarrowVecsTop : kLpNarrowVecs)) AURORA_LOGPROB(LpNarrow);
-  else AURORA_LOGPROB(LpWide);
+  const int64_t vecs = P.V / LpType<T>::kV;
+  if ((vecs + P.splits - 1) / P.splits <= kLpHeld * LpWide::kStep && P.rows <= kLpFewRows) AURORA_LOGPROB(LpWide, kLpHeld);
+  else if (P.splits == 1 && P.rows >= kLpNarrowRows && vecs <= (P.n_top > 0 ? kLpNarrowVecsTop : kLpNarrowVecs)) AURORA_LOGPROB(LpNarrow, 0);
+  else AURORA_LOGPROB(LpWide, 0);
 #undef AURORA_LOGPROB
   if (hipError_t e = hipGetLastError(); e != hipSuccess || P.splits == 1) return e;
   hipLaunchKernelGGL(logprob_merge_kernel<T>, logprob_grid(P.rows), dim3(kLpMergeThreads), 0, st, P);
