@@ -26,6 +26,7 @@ constexpr int kPlanThreads = 256;
 constexpr int kPlanPer = 4;                              // requests a thread
 constexpr int kPlanChunk = kPlanThreads * kPlanPer;      // requests planned at a time
 constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanFewRows = 1 << 18;                    // up to here a thread writes one row, beyond four
 
 // What the writing needs: per request the first row, page taken and page given back, the tokens held, and the table column at which
 // the pages taken or given back start; then the stack's size and the totals.
@@ -37,7 +38,11 @@ struct PlanReq { int held, want, col, need, back; unsigned rows; bool grow, shri
 // Sums of rows stop at 2^32 - 1, past every limit: no order of adding changes them, and one that stopped is refused.
 __device__ __forceinline__ unsigned add_rows(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
 
-__device__ __forceinline__ int pages_of(int tokens, int page) { return (int)(((unsigned)tokens + (unsigned)page - 1u) / (unsigned)page); }
+// (a division costs as much as the rest of a request: pages of a power of two shift)
+__device__ __forceinline__ int page_of(const CachePlanLaunch& P, unsigned token) {
+  return (int)(P.page_shift >= 0 ? token >> P.page_shift : token / (unsigned)P.page);
+}
+__device__ __forceinline__ int pages_of(const CachePlanLaunch& P, int tokens) { return page_of(P, (unsigned)tokens + (unsigned)P.page - 1u); }
 
 __device__ __forceinline__ PlanReq plan_request(const CachePlanLaunch& P, int b) {
   PlanReq r = {};
@@ -46,7 +51,7 @@ __device__ __forceinline__ PlanReq plan_request(const CachePlanLaunch& P, int b)
   r.want = P.want_lens[b];
   r.differs = r.want != r.held;
   if (r.held < 0 || r.want < 0) return r;
-  const int hp = pages_of(r.held, P.page), wp = pages_of(r.want, P.page);
+  const int hp = pages_of(P, r.held), wp = pages_of(P, r.want);
   if (hp > P.max_pages || wp > P.max_pages) return r;
   r.grow = r.want > r.held;
   r.shrink = r.want < r.held;
@@ -152,19 +157,32 @@ __device__ __forceinline__ PlanTotals plan_requests(const CachePlanLaunch& P, co
     }
     if (refused) atomicAdd(&s_refused, refused);
     PlanSums cum = at;
+    int row[kPlanPer], take[kPlanPer], give[kPlanPer];
 #pragma unroll
     for (int i = 0; i < kPlanPer; ++i) {
       const int b = base + tid * kPlanPer + i;
+      const bool past = b >= cut;
+      row[i] = (int)(past ? cut_rows : cum.rows);
+      take[i] = past ? cut_need : cum.need;
+      give[i] = cum.back;
       if (b < P.B) {
-        const bool past = b >= cut;
-        const int row = (int)(past ? cut_rows : cum.rows);
-        A.row[b] = row; A.take[b] = past ? cut_need : cum.need; A.give[b] = cum.back; A.held[b] = r[i].held; A.col[b] = r[i].col;
+        if constexpr (!kOneChunk) {
+          A.row[b] = row[i]; A.take[b] = take[i]; A.give[b] = give[i]; A.held[b] = r[i].held; A.col[b] = r[i].col;
+        }
         if (publish) {
           P.seq_lens[b] = r[i].shrink || (r[i].grow && !past) ? r[i].want : r[i].held;
-          if (P.row_start) P.row_start[b] = row;
+          if (P.row_start) P.row_start[b] = row[i];
         }
       }
       cum.back += r[i].back; cum.need += r[i].need; cum.rows = add_rows(cum.rows, r[i].rows);
+    }
+    if constexpr (kOneChunk) {  // in LDS, past the last request too: there the sums are the totals
+      static_assert(kPlanPer == 4, "one vector an array");
+      ((int4*)A.row)[tid] = make_int4(row[0], row[1], row[2], row[3]);
+      ((int4*)A.take)[tid] = make_int4(take[0], take[1], take[2], take[3]);
+      ((int4*)A.give)[tid] = make_int4(give[0], give[1], give[2], give[3]);
+      ((int4*)A.held)[tid] = make_int4(r[0].held, r[1].held, r[2].held, r[3].held);
+      ((int4*)A.col)[tid] = make_int4(r[0].col, r[1].col, r[2].col, r[3].col);
     }
   }
   PlanTotals t;
@@ -172,7 +190,7 @@ __device__ __forceinline__ PlanTotals plan_requests(const CachePlanLaunch& P, co
   t.freed = freed;
   t.taken = cut != INT32_MAX ? cut_need : carry.need;
   t.rows = (int)(cut != INT32_MAX ? cut_rows : carry.rows);
-  if (tid == 0) { A.row[P.B] = t.rows; A.take[P.B] = t.taken; A.give[P.B] = t.freed; }
+  if (tid == 0 && (!kOneChunk || P.B == kPlanChunk)) { A.row[P.B] = t.rows; A.take[P.B] = t.taken; A.give[P.B] = t.freed; }
   __syncthreads();
   if (publish && tid == 0) {
     if (P.row_start) P.row_start[P.B] = t.rows;
@@ -203,59 +221,69 @@ __device__ __forceinline__ int taken_page(const CachePlanLaunch& P, const PlanAr
   return k < t.freed ? given_page(P, A, t.freed - 1 - k) : P.free_pages[t.n - 1 - (k - t.freed)];
 }
 
-// the table cells, stack entries and rows of this workgroup
-__device__ __forceinline__ void plan_write(const CachePlanLaunch& P, const PlanArrays& A, const PlanTotals& t) {
-  const int first = blockIdx.x * kPlanThreads + threadIdx.x, step = gridDim.x * kPlanThreads;
-  for (int k = first; k < t.taken; k += step) {
-    const int b = plan_owner(A.take, P.B, k);
-    P.block_table[(size_t)b * P.max_pages + A.col[b] + (k - A.take[b])] = taken_page(P, A, t, k);
-  }
-  for (int j = first; j < t.freed - t.taken; j += step)
-    if ((int64_t)t.n + j < P.num_pages) P.free_pages[t.n + j] = given_page(P, A, j);
-  if (!P.slots) return;
-  // four rows a thread: one search, one page for all of them more often than not
-  for (int64_t r0 = (int64_t)first * 4; r0 < P.max_rows; r0 += (int64_t)step * 4) {
-    int pos[4], slot[4];
-    int b = 0, left = 0, at = 0, pg = 0, off = 0, pid = 0;  // left: rows of request b from here on
+// kRows rows, with one search and one page for all of them more often than not
+template <int kRows>
+__device__ __forceinline__ void plan_rows(const CachePlanLaunch& P, const PlanArrays& A, const PlanTotals& t, int64_t r0) {
+  int pos[kRows], slot[kRows];
+  int b = 0, left = 0, at = 0, pg = 0, off = 0, pid = 0;  // left: rows of request b from here on
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = (int)r0 + e;
-      if (r >= t.rows) { pos[e] = 0; slot[e] = -1; continue; }
-      const bool enter = left == 0;
-      if (enter) {
-        b = plan_owner(A.row, P.B, r);
-        left = A.row[b + 1] - r;
-        at = A.held[b] + (r - A.row[b]);
-        pg = at / P.page;
-        off = at - pg * P.page;
-      } else if (off == P.page) {
-        ++pg;
-        off = 0;
-      }
-      if (enter || off == 0) {
-        const int col = A.col[b];
-        pid = pg < col ? P.block_table[(size_t)b * P.max_pages + pg] : taken_page(P, A, t, A.take[b] + pg - col);
-      }
-      pos[e] = at++;
-      slot[e] = (int)((unsigned)pid * (unsigned)P.page + (unsigned)off++);
-      --left;
+  for (int e = 0; e < kRows; ++e) {
+    const int r = (int)r0 + e;
+    if (r >= t.rows) { pos[e] = 0; slot[e] = -1; continue; }
+    const bool enter = left == 0;
+    if (enter) {
+      b = plan_owner(A.row, P.B, r);
+      left = A.row[b + 1] - r;
+      at = A.held[b] + (r - A.row[b]);
+      pg = page_of(P, at);
+      off = at - pg * P.page;
+    } else if (off == P.page) {
+      ++pg;
+      off = 0;
     }
-    if (P.wide_rows && r0 + 4 <= P.max_rows) {
-      *(int4*)(P.positions + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-      *(int4*)(P.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
-    } else {
+    if (enter || off == 0) {
+      const int col = A.col[b];
+      pid = pg < col ? P.block_table[(size_t)b * P.max_pages + pg] : taken_page(P, A, t, A.take[b] + pg - col);
+    }
+    pos[e] = at++;
+    slot[e] = (int)((unsigned)pid * (unsigned)P.page + (unsigned)off++);
+    --left;
+  }
+  if (kRows == 4 && P.wide_rows && r0 + 4 <= P.max_rows) {
+    *(int4*)(P.positions + r0) = make_int4(pos[0], pos[1 % kRows], pos[2 % kRows], pos[3 % kRows]);
+    *(int4*)(P.slots + r0) = make_int4(slot[0], slot[1 % kRows], slot[2 % kRows], slot[3 % kRows]);
+  } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (r0 + e < P.max_rows) { P.positions[r0 + e] = pos[e]; P.slots[r0 + e] = slot[e]; }
+    for (int e = 0; e < kRows; ++e)
+      if (r0 + e < P.max_rows) { P.positions[r0 + e] = pos[e]; P.slots[r0 + e] = slot[e]; }
+  }
+}
+
+// The rows, table cells and stack entries of this workgroup: each is a chain of a search and one or two loads, so they are numbered
+// through, and a thread goes through as few of them as the launch allows.
+template <int kRows>
+__device__ __forceinline__ void plan_write(const CachePlanLaunch& P, const PlanArrays& A, const PlanTotals& t) {
+  const int64_t rows = P.slots ? ((int64_t)P.max_rows + kRows - 1) / kRows : 0, takes = rows + t.taken, all = takes + max(0, t.freed - t.taken);
+  for (int64_t i = (int64_t)blockIdx.x * kPlanThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kPlanThreads) {
+    if (i < rows) {
+      plan_rows<kRows>(P, A, t, kRows * i);
+    } else if (i < takes) {
+      const int k = (int)(i - rows), b = plan_owner(A.take, P.B, k);
+      P.block_table[(size_t)b * P.max_pages + A.col[b] + (k - A.take[b])] = taken_page(P, A, t, k);
+    } else {
+      const int j = (int)(i - takes);
+      if ((int64_t)t.n + j < P.num_pages) P.free_pages[t.n + j] = given_page(P, A, j);
     }
   }
 }
 
+template <int kRows>
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanLaunch P) {
-  __shared__ int32_t s_row[kPlanChunk + 1], s_take[kPlanChunk + 1], s_give[kPlanChunk + 1], s_held[kPlanChunk], s_col[kPlanChunk];
+  __shared__ __attribute__((aligned(16))) int32_t s_row[kPlanChunk + 4], s_take[kPlanChunk + 4], s_give[kPlanChunk + 4], s_held[kPlanChunk],
+      s_col[kPlanChunk];
   const PlanArrays A = {s_row, s_take, s_give, s_held, s_col};
   const PlanTotals t = plan_requests<true>(P, A, blockIdx.x == 0);
-  plan_write(P, A, t);
+  plan_write<kRows>(P, A, t);
 }
 
 __device__ __forceinline__ PlanArrays workspace_arrays(const CachePlanLaunch& P) {
@@ -269,20 +297,25 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_requests_kernel(Cache
 }
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_write_kernel(CachePlanLaunch P) {
   const int4 t = *(const int4*)P.work;
-  plan_write(P, workspace_arrays(P), PlanTotals{t.x, t.y, t.z, t.w});
+  plan_write<4>(P, workspace_arrays(P), PlanTotals{t.x, t.y, t.z, t.w});
 }
 
 size_t cache_plan_work_bytes(int batch) { return 16 + 5 * ((size_t)batch + 1) * sizeof(int32_t); }
 
-hipError_t launch_cache_plan(const CachePlanLaunch& P, hipStream_t st) {
-  // A workgroup per 1024 rows or 4096 cells of the table, whichever asks for more (how many cells change hands only the lengths say).
-  const int64_t rows = P.slots ? ((int64_t)P.max_rows + 1023) / 1024 : 0;
-  const int64_t cells = ((int64_t)P.B * P.max_pages + 4095) / 4096;
-  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(rows, cells), 1024));
+hipError_t launch_cache_plan(const CachePlanLaunch& plan, hipStream_t st) {
+  CachePlanLaunch P = plan;
+  P.page_shift = (P.page & (P.page - 1)) == 0 ? __builtin_ctz(P.page) : -1;
+  // Few rows are given a thread each: four that belong to two or three requests are as many loads in turn.  A workgroup per 256 or 1024
+  // rows, and per 4096 cells of the table (how many cells change hands only the lengths say).
+  const bool few = P.max_rows <= kPlanFewRows;
+  const int64_t rows = P.slots ? ((int64_t)P.max_rows + (few ? 255 : 1023)) / (few ? 256 : 1024) : 0;
+  const int64_t cells = (int64_t)P.B * P.max_pages / 4096;
+  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(rows + cells, 1024));
   // an output that replaces an input is safe within one workgroup alone: the others read the input too
   const bool in_place = P.free_count_out == P.free_count || P.seq_lens == P.held_lens || P.seq_lens == P.want_lens;
   if (P.B <= kPlanChunk && (grid == 1 || !in_place)) {
-    hipLaunchKernelGGL(cache_plan_kernel, dim3(grid), dim3(kPlanThreads), 0, st, P);
+    if (few) hipLaunchKernelGGL(cache_plan_kernel<1>, dim3(grid), dim3(kPlanThreads), 0, st, P);
+    else hipLaunchKernelGGL(cache_plan_kernel<4>, dim3(grid), dim3(kPlanThreads), 0, st, P);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(cache_plan_requests_kernel, dim3(1), dim3(kPlanThreads), 0, st, P);

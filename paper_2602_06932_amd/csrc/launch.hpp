@@ -162,6 +162,7 @@ hipError_t launch_check_inputs(const CheckLaunch& c, hipStream_t st);
 // block tables and slot maps from request lengths (see cache_plan.hip)
 struct CachePlanLaunch {
   int B, page, max_pages, num_pages, max_rows;
+  int page_shift;                                          // set by the launcher: page = 1 << page_shift, or -1
   bool wide_rows;                                          // positions and slots start at 16 bytes
   const int32_t *held_lens, *want_lens, *free_count;       // held_lens may be NULL
   int32_t *block_table, *free_pages, *free_count_out, *seq_lens;
