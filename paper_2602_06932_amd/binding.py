@@ -106,8 +106,10 @@ def load():
     # One HIP runtime per process: PyTorch ships its own copy of the runtime library, and device pointers and
     # streams made by one copy mean nothing to another.  Importing torch first makes the loader resolve this
     # library's dependency to the copy torch has already mapped, whatever order the caller imports things in.
+    global _contiguous, _address
     try:
-        import torch  # noqa: F401
+        import torch
+        _contiguous, _address = torch.Tensor.is_contiguous, torch.Tensor.data_ptr
     except ImportError:
         pass
     lib = C.CDLL(LIB_PATH)
@@ -191,22 +193,36 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_contiguous = _address = None  # of torch's tensors, once it is there (load())
+
+
+def _ptrs(*ts):
+    """_ptr of each; tensors all of them, as in most calls, take less time so."""
+    try:
+        if all(map(_contiguous, ts)):
+            return map(_address, ts)
+    except TypeError:  # None or an address among them
+        pass
+    return map(_ptr, ts)
+
+
 def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
     """Device address of a tensor whose rows (dimension 0) may lie apart, as the descriptor's stride says."""
     if t is None or t.__class__ is int:
         return t
-    s = t.stride()
-    if s[0] == stride and len(s) == 3 and s[2] == 1 and s[1] == t.size(2):  # what a view of a fused projection's output is
-        return t.data_ptr()
     if stride == 0 and t.is_contiguous():
         return t.data_ptr()
-    n, dense = t.shape, 1
-    for k in range(len(n) - 1, 0, -1):
-        if s[k] != dense and n[k] > 1:
-            raise ValueError(f"{name}: the elements of a row must be contiguous")
-        dense *= n[k]
-    if s[0] != (stride or dense) and n[0] > 1:
-        raise ValueError(f"{name}: rows are {s[0]} elements apart, the descriptor says {stride or dense}")
+    s, n = t.stride(), t.shape
+    if stride == n[-1] and t.is_contiguous():  # rows over all dimensions but the last
+        return t.data_ptr()
+    if len(s) != 3 or s[0] != stride or s[2] != 1 or s[1] != n[2]:  # (not simply a view of a fused projection's output)
+        dense = 1
+        for k in range(len(n) - 1, 0, -1):
+            if s[k] != dense and n[k] > 1:
+                raise ValueError(f"{name}: the elements of a row must be contiguous")
+            dense *= n[k]
+        if s[0] != (stride or dense) and n[0] > 1:
+            raise ValueError(f"{name}: rows are {s[0]} elements apart, the descriptor says {stride or dense}")
     return t.data_ptr()
 
 
@@ -385,10 +401,9 @@ def aurora_cache_plan_workspace_bytes(desc) -> int:
 
 def aurora_cache_plan(desc, held_lens, want_lens, block_table, free_pages, free_count, free_count_out, seq_lens, row_start,
                       positions, slots, info, workspace, stream=None, check=True) -> int:
-    wb = workspace.numel() * workspace.element_size()
-    st = load().aurora_cache_plan(_ref(desc), _ptr(held_lens), _ptr(want_lens), _ptr(block_table), _ptr(free_pages),
-                                  _ptr(free_count), _ptr(free_count_out), _ptr(seq_lens), _ptr(row_start), _ptr(positions),
-                                  _ptr(slots), _ptr(info), _ptr(workspace), wb, _stream(stream))
+    st = load().aurora_cache_plan(_ref(desc), *_ptrs(held_lens, want_lens, block_table, free_pages, free_count, free_count_out,
+                                                     seq_lens, row_start, positions, slots, info, workspace),
+                                  workspace.nbytes, _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_cache_plan")
     return st
@@ -396,9 +411,11 @@ def aurora_cache_plan(desc, held_lens, want_lens, block_table, free_pages, free_
 
 def aurora_rope_append(desc, q, k, v, positions, slots, frequencies, q_out, k_pages, v_pages, stream=None, check=True) -> int:
     """q, k, v and q_out may be tensors whose rows lie apart (views of a fused projection's output): their strides are the descriptor's."""
-    st = load().aurora_rope_append(_ref(desc), _rows_ptr(q, desc.q_stride, "q"), _rows_ptr(k, desc.k_stride, "k"),
-                                   _rows_ptr(v, desc.v_stride, "v"), _ptr(positions), _ptr(slots), _ptr(frequencies),
-                                   _rows_ptr(q_out, desc.q_out_stride, "q_out"), _ptr(k_pages), _ptr(v_pages), _stream(stream))
+    lib = load()
+    pos, sl, fr, kp, vp = _ptrs(positions, slots, frequencies, k_pages, v_pages)
+    st = lib.aurora_rope_append(_ref(desc), _rows_ptr(q, desc.q_stride, "q"), _rows_ptr(k, desc.k_stride, "k"),
+                                _rows_ptr(v, desc.v_stride, "v"), pos, sl, fr, _rows_ptr(q_out, desc.q_out_stride, "q_out"), kp, vp,
+                                _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_rope_append")
     return st
@@ -406,8 +423,8 @@ def aurora_rope_append(desc, q, k, v, positions, slots, frequencies, q_out, k_pa
 
 def aurora_rope_append_backward(desc, dq_out, dk_pages, dv_pages, positions, slots, frequencies, dq, dk, dv, stream=None,
                                 check=True) -> int:
-    st = load().aurora_rope_append_backward(_ref(desc), _rows_ptr(dq_out, desc.q_out_stride, "dq_out"), _ptr(dk_pages), _ptr(dv_pages),
-                                            _ptr(positions), _ptr(slots), _ptr(frequencies), _rows_ptr(dq, desc.q_stride, "dq"),
+    st = load().aurora_rope_append_backward(_ref(desc), _rows_ptr(dq_out, desc.q_out_stride, "dq_out"),
+                                            *_ptrs(dk_pages, dv_pages, positions, slots, frequencies), _rows_ptr(dq, desc.q_stride, "dq"),
                                             _rows_ptr(dk, desc.k_stride, "dk"), _rows_ptr(dv, desc.v_stride, "dv"), _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_rope_append_backward")
@@ -434,9 +451,8 @@ def aurora_token_logprobs_workspace_bytes(desc) -> int:
 def aurora_token_logprobs(desc, logits, tokens, logprob, entropy, lse, top_ids, top_logprobs, workspace, stream=None,
                           check=True) -> int:
     """`logits` may be a tensor (its rows may lie apart) or a raw device address (int), e.g. from aurora_verify_logits_ptr()."""
-    wb = workspace.numel() * workspace.element_size()
-    st = load().aurora_token_logprobs(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"), _ptr(tokens), _ptr(logprob),
-                                      _ptr(entropy), _ptr(lse), _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), wb,
+    st = load().aurora_token_logprobs(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"),
+                                      *_ptrs(tokens, logprob, entropy, lse, top_ids, top_logprobs, workspace), workspace.nbytes,
                                       _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_token_logprobs")
@@ -444,8 +460,8 @@ def aurora_token_logprobs(desc, logits, tokens, logprob, entropy, lse, top_ids, 
 
 
 def aurora_token_logprobs_backward(desc, logits, tokens, entropy, lse, dlogprob, dentropy, dlogits, stream=None, check=True) -> int:
-    st = load().aurora_token_logprobs_backward(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"), _ptr(tokens), _ptr(entropy),
-                                               _ptr(lse), _ptr(dlogprob), _ptr(dentropy),
+    st = load().aurora_token_logprobs_backward(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"),
+                                               *_ptrs(tokens, entropy, lse, dlogprob, dentropy),
                                                _rows_ptr(dlogits, desc.row_stride, "dlogits"), _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_token_logprobs_backward")

@@ -5,6 +5,7 @@
 
 #include <math.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <mutex>
 
@@ -696,10 +697,10 @@ int check_logprob(const aurora_logprob_desc* d) {
 }
 
 struct LogprobPlan { int splits; size_t keys_off, bytes; };
-LogprobPlan plan_logprob(const aurora_logprob_desc* d) {
+LogprobPlan plan_logprob(const aurora_logprob_desc* d, int rows) {
   LogprobPlan p = {};
-  p.splits = logprob_splits(d->rows, d->vocab, d->dtype == AURORA_BF16);
-  const size_t parts = p.splits > 1 ? (size_t)d->rows * p.splits : 0;
+  p.splits = logprob_splits(rows, d->vocab, d->dtype == AURORA_BF16);
+  const size_t parts = p.splits > 1 ? (size_t)rows * p.splits : 0;
   p.keys_off = align_up(parts * sizeof(LogprobPart));
   p.bytes = p.keys_off + align_up(parts * d->n_top * sizeof(unsigned long long));
   if (p.bytes < 256) p.bytes = 256;
@@ -818,7 +819,8 @@ int aurora_token_logprobs_workspace_bytes(const aurora_logprob_desc* desc, size_
   if (!out_bytes) return AURORA_ERR_INVALID_ARG;
   int rc = check_logprob(desc);
   if (rc != AURORA_OK) return rc;
-  *out_bytes = plan_logprob(desc).bytes;
+  // few rows are cut into parts where many are not: what is enough for many is enough for any less
+  *out_bytes = std::max(plan_logprob(desc, desc->rows).bytes, plan_logprob(desc, std::min<int>(desc->rows, logprob_few_rows())).bytes);
   return AURORA_OK;
 }
 
@@ -833,7 +835,7 @@ int aurora_token_logprobs(const aurora_logprob_desc* d, const void* logits, cons
   for (const void* p : {(const void*)tokens, (const void*)logprob, (const void*)entropy, (const void*)lse, (const void*)top_ids,
                         (const void*)top_logprobs, (const void*)d->temperatures})
     if (unaligned(p, 4)) return AURORA_ERR_INVALID_ARG;
-  const LogprobPlan plan = plan_logprob(d);
+  const LogprobPlan plan = plan_logprob(d, d->rows);
   if (!workspace || misaligned(workspace) || workspace_bytes < plan.bytes) return AURORA_ERR_WORKSPACE;
   if (!have_device()) return AURORA_ERR_HIP;
   LogprobLaunch a = logprob_launch_from(d);

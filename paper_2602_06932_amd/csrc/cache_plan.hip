@@ -228,8 +228,8 @@ __device__ __forceinline__ void plan_rows(const CachePlanLaunch& P, const PlanAr
   int b = 0, left = 0, at = 0, pg = 0, off = 0, pid = 0;  // left: rows of request b from here on
 #pragma unroll
   for (int e = 0; e < kRows; ++e) {
+    if (r0 + e >= t.rows) { pos[e] = 0; slot[e] = -1; continue; }
     const int r = (int)r0 + e;
-    if (r >= t.rows) { pos[e] = 0; slot[e] = -1; continue; }
     const bool enter = left == 0;
     if (enter) {
       b = plan_owner(A.row, P.B, r);

@@ -768,6 +768,7 @@ int logprob_splits(int64_t rows, int V, bool bf16) {
   const int64_t vecs = V / (bf16 ? 8 : 4), least = (vecs + most - 1) / most, want = (vecs + held - 1) / held;
   return (int)std::max<int64_t>(rows <= kLpFewRows && want <= kLpMaxSplits ? want : least, 1);
 }
+int logprob_few_rows() { return kLpFewRows; }
 int logprob_max_top() { return kLpMaxTop; }
 int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kStep * 4; }
 

@@ -129,6 +129,23 @@ def test_a_long_prefill_and_its_end(gpu_lib):
     _check(gpu_lib, want, done, ref["table"], ref["free"], ref["count"], page, None, in_place=True)
 
 
+def test_as_many_rows_as_there_can_be(gpu_lib):
+    """The padding of 2^31 - 1 rows: their numbers stay within 32 bits."""
+    av = gpu_lib
+    rows = 2 ** 31 - 1
+    d = av.aurora_cache_plan_desc(batch=2, page_size=16, max_pages_per_seq=4, num_pages=9, max_rows=rows)
+    dev = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    table, free, lens = torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), torch.arange(9, dtype=torch.int32, device="cuda"), dev(0, 0)
+    positions, slots = (torch.full((rows,), 7, dtype=torch.int32, device="cuda") for _ in range(2))
+    ws = torch.empty(av.aurora_cache_plan_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    count = dev(9)
+    av.aurora_cache_plan(d, None, dev(3, 17), table, free, count, count, lens, None, positions, slots, None, ws)
+    torch.cuda.synchronize()
+    assert lens.tolist() == [3, 17] and int(count) == 6 and table.tolist() == [[8, -1, -1, -1], [7, 6, -1, -1]]
+    assert slots[:20].tolist() == [128, 129, 130] + list(range(112, 128)) + [96] and positions[:20].tolist() == [0, 1, 2] + list(range(17))
+    assert int(slots[20:].max()) == -1 and int(slots[20:].min()) == -1 and int(positions[20:].max()) == 0 and int(positions[20:].min()) == 0
+
+
 def test_a_call_may_be_repeated_and_captured(gpu_lib):
     """Distinct outputs: the same call on the same state gives the same result, also from a graph that is replayed on new lengths."""
     av = gpu_lib

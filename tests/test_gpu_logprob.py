@@ -172,6 +172,26 @@ def test_rows_longer_than_a_workgroup_takes(gpu_lib):
     _check(gpu_lib, z, [12345678], 1.0, 32, grad=False)
 
 
+def test_more_rows_than_a_launch_counts_in_one_dimension(gpu_lib):
+    av = gpu_lib
+    M, V = (1 << 22) + 5, 3
+    z = torch.randn(M, V, device="cuda")
+    tok = torch.randint(0, V, (M,), device="cuda", dtype=torch.int32)
+    d = av.aurora_logprob_desc(rows=M, vocab=V, dtype=av.AURORA_F32, n_top=1)
+    ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    lp, H, lse, tl = (torch.full((M,), 7.0, device="cuda") for _ in range(4))
+    ti, g = torch.full((M,), -7, dtype=torch.int32, device="cuda"), torch.zeros_like(z)
+    av.aurora_token_logprobs(d, z.view(1, M, V), tok, lp, H, lse, ti, tl, ws)
+    av.aurora_token_logprobs_backward(d, z, tok, None, lse, torch.ones(M, device="cuda"), None, g)
+    torch.cuda.synchronize()
+    ref = torch.log_softmax(z.double(), -1)
+    # three values: every sum within a few ulp of numbers below 16
+    assert (lp - ref.gather(1, tok.long()[:, None])[:, 0]).abs().max() < 4e-6
+    assert (H + (ref.exp() * ref).sum(1)).abs().max() < 4e-6 and torch.equal(ti, z.argmax(1).to(torch.int32))
+    want = torch.nn.functional.one_hot(tok.long(), V) - ref.exp()
+    assert (g - want).abs().max() < 4e-6
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shift", [0, 1, 3])
 def test_rows_apart_and_not_aligned(gpu_lib, shift, dtype):

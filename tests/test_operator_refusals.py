@@ -116,6 +116,14 @@ def test_logprob_descriptors(desc, want):
         av.aurora_token_logprobs_workspace_bytes(_desc(av.aurora_logprob_desc, LP, **desc))
 
 
+def test_a_logprob_workspace_is_enough_for_fewer_rows():
+    for dtype in (av.AURORA_F32, av.AURORA_BF16):
+        for vocab in (777, 32000, 200064, 1 << 24):
+            n = [av.aurora_token_logprobs_workspace_bytes(_desc(av.aurora_logprob_desc, LP, rows=r, vocab=vocab, dtype=dtype, n_top=32))
+                 for r in (0, 1, 5, 100, 640, 641, 1000, 1024, 5000, 100000)]
+            assert n == sorted(n) and all(x % 256 == 0 and x for x in n)
+
+
 def test_logprob_arguments():
     assert _lp(logits=None) == BAD and _lp(tokens=None) == BAD and _lp(logprob=None) == BAD and _lp(ids=None) == BAD and _lp(tops=None) == BAD
     assert _lp(dict(n_top=0), tokens=None, logprob=None, entropy=None, lse=None) == BAD     # nothing requested
