@@ -4,7 +4,7 @@
 //   lse = log sum_v e^x_v     logprob = x_t - lse     H = lse - sum_v p_v x_v     p_v = e^(x_v - lse)
 //   dz_v = [ g_l (delta_vt - p_v) - g_H p_v (log p_v + H) ] / T
 //
-// Forward: bound by the one read of the logits.  A thread keeps the largest logit m so far, the reference r of it, s = sum e^(x - r) and
+// Forward: bound by the one read of the logits.  A thread keeps a logit m near the largest so far, the reference r of it, s = sum e^(x - r) and
 // t = sum (x - r) e^(x - r), in units of log 2, so that H = log s - t / s takes no second pass; moving the reference by d turns (s, t)
 // into (s, t + d s) 2^d.  Sixteen or 32 elements are summed in 32 bits at a time, their sums in 64: a row may have a million
 // entries.  r is the value that was really subtracted, rounded as it is, and the outputs are formed from it, so that its rounding
@@ -42,11 +42,28 @@ constexpr int kLpMaxSplits = 64;
 constexpr float kLpLog2e = 1.4426950408889634f;
 constexpr double kLpLn2 = 0.69314718055994530942;
 constexpr float kLpFloor = -1e4f;  // stands in for -inf times zero: 2^-10000 is zero as well
+// The reference only moves when a logit is so many bits above it: exponentials stay below 2^8, as exact as below 1, and the move - 60
+// instructions, of which some lane of a wavefront has need in nearly every step if every new maximum counts - becomes rare
+// (1280 x 200064 bf16: 10.7 vector instructions an element, the units 97 % busy -> 7.3).
+constexpr float kLpLazyBits = 8.f;
 constexpr int kLpGridRows = 1 << 22;
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+
+// the largest, and the smallest, of three as they were loaded (fmaxf would first make quiet numbers of them, an instruction each)
+__device__ __forceinline__ float lp_max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+__device__ __forceinline__ float lp_min3(float a, float b, float c) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 template <typename T> struct LpType { static constexpr int kV = 16 / (int)sizeof(T); };
 
@@ -352,43 +369,40 @@ __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int ste
   }
   int have = min(count, n);
   if (ties && have < n) {
-    // Equal values in the order of their ids: the row's pieces in order, in each the lowest id not yet taken.
+    // Equal values in the order of their ids: the row's pieces in order, in each the lowest id not yet taken.  A thread's equal elements of
+    // a piece are bits, in the order of their ids.
+    static_assert(kLpVecs * kV <= 32, "a bit an element");
     const float at = lp_value(bound);
     for (int piece = -1; piece <= steps && have < n; ++piece) {
-      int ids[kLpVecs * kV];
-      int m = 0;
-      if (piece < 0 || piece == steps) {  // the elements before, and after, the vectors
-        const int id = (piece < 0 ? w.lo : w.tail) + tid;
-        ids[0] = id < (piece < 0 ? w.first : w.hi) && to_f32<T>(row[id]) == at ? id : INT32_MAX;
-        m = 1;
+      const bool outside = piece < 0 || piece == steps;  // the elements before, and after, the vectors
+      const int first = outside ? (piece < 0 ? w.lo : w.tail) + tid : w.first + (piece * S::kStep + tid) * kV;
+      unsigned equal = 0;
+      if (outside) {
+        equal = first < (piece < 0 ? w.first : w.hi) && to_f32<T>(row[first]) == at ? 1u : 0u;
       } else {
 #pragma unroll
         for (int u = 0; u < kLpVecs; ++u) {
-          const int vec = piece * S::kStep + u * S::kThreads + tid;
+          if (piece * S::kStep + u * S::kThreads + tid >= w.vecs) break;
+          float x[kV];
+          lp_widen<T>(*(const u32x4_t*)(row + first + u * S::kThreads * kV), x);
 #pragma unroll
-          for (int e = 0; e < kV; ++e) {
-            const int id = w.first + vec * kV + e;
-            ids[u * kV + e] = vec < w.vecs && to_f32<T>(row[id]) == at ? id : INT32_MAX;
-          }
+          for (int e = 0; e < kV; ++e) equal |= x[e] == at ? 1u << (u * kV + e) : 0u;
         }
-        m = kLpVecs * kV;
       }
-      int last = -1;
       while (have < n) {
-        int low = INT32_MAX;
-#pragma unroll
-        for (int i = 0; i < kLpVecs * kV; ++i)
-          if (i < m && ids[i] > last) low = min(low, ids[i]);
-        low = wave_min(low);
+        const int bit = __ffs(equal) - 1, mine = equal ? first + bit / kV * S::kThreads * kV + bit % kV : INT32_MAX;
+        int low = wave_min(mine);
         __syncthreads();
         if (lane == 0) L.best[wave] = low;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < S::kWaves; ++i) low = min(low, L.best[i]);
         if (low == INT32_MAX) break;
-        if (tid == 0) out(have, lp_key(at, low));
+        if (mine == low) {
+          out(have, lp_key(at, low));
+          equal &= equal - 1;
+        }
         ++have;
-        last = low;
       }
     }
   }
@@ -415,7 +429,11 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   const int steps = (w.vecs + S::kStep - 1) / S::kStep;
   const u32x4_t* vp = (const u32x4_t*)(z + w.first);
 
-  u32x4_t cur[kHeld > 0 ? kHeld : 1][kLpVecs];
+  // Two elements a word are as many instructions a byte again: 16-bit rows are bound by them (7.3 an element, the units 90 % busy), so
+  // that two buffers that need no moves, and one test a step in place of one an element, pay.  fp32 rows are slower for both (4096 x
+  // 32000 83 -> 87 us: 144 registers).
+  constexpr bool kTight = sizeof(T) == 2;
+  u32x4_t cur[kHeld > 0 ? kHeld : kTight ? 2 : 1][kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
 #pragma unroll
     for (int u = 0; u < kLpVecs; ++u) v[u] = __builtin_nontemporal_load(vp + min(step * S::kStep + u * S::kThreads + tid, w.vecs - 1));
@@ -435,35 +453,44 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   LpSums mine = {-INFINITY, 0.0, 0.0};
   float col = -INFINITY;
   float neg = 0.f;  // minus the reference
+  const float lazy = kLpLazyBits / c, lowest = -kLpFar / c;
   bool far = false;
-  // takes elements into the running sums (top: their maximum)
-  auto add = [&](auto& x, float top) {
+  // takes elements into the running sums (top, low: the largest and the smallest).  0 times -inf must not get into t: where there is
+  // one, or a value whose x would be, distances stop at the floor.
+  auto sums = [&](const auto& x, auto floor) {
     constexpr int n = (int)(sizeof(x) / sizeof(float));
-    if (top > mine.m) {
-      mine = lp_moved(mine, top, c);
-      neg = -(mine.m * c);
-      far = lp_far(mine.m, c);
-    }
-    if (far) {
-#pragma unroll
-      for (int i = 0; i < n; ++i) x[i] -= mine.m;
-      neg = 0.f;
-    }
     float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < n; ++i) {
       const float d = fmaf(x[i], c, neg);
       const float e = __builtin_amdgcn_exp2f(d);
       s[i & 3] += e;
-      t[i & 3] = fmaf(e, fmaxf(d, kLpFloor), t[i & 3]);
+      t[i & 3] = fmaf(e, decltype(floor)::value ? fmaxf(d, kLpFloor) : d, t[i & 3]);
     }
     mine.s += (double)((s[0] + s[1]) + (s[2] + s[3]));
     mine.t += (double)((t[0] + t[1]) + (t[2] + t[3]));
   };
+  auto add = [&](auto& x, float top, float low) {
+    constexpr int n = (int)(sizeof(x) / sizeof(float));
+    if (top > mine.m + lazy) {
+      asm volatile("");  // (what follows is rare: not to be worked out ahead of the test)
+      mine = lp_moved(mine, top, c);
+      neg = -(mine.m * c);
+      far = lp_far(mine.m, c);
+    }
+    if (far) {
+      asm volatile("");
+#pragma unroll
+      for (int i = 0; i < n; ++i) x[i] -= mine.m;
+      neg = 0.f;
+    }
+    if (!kTight || far || low < lowest) sums(x, std::true_type{});
+    else sums(x, std::false_type{});
+  };
 
   // one step's elements, the next step's already on their way; kWhole: no vector of the step lies past the part
   float tops[kHeld > 0 ? kHeld : 1];  // a held step's maximum
-  auto take = [&](int step, u32x4_t (&v)[kLpVecs], float& held_top, auto whole) {
+  auto take = [&](int step, u32x4_t (&v)[kLpVecs], u32x4_t (&next)[kLpVecs], float& held_top, auto whole) {
     constexpr bool kWhole = decltype(whole)::value;
     float x[kLpVecs * kV];
 #pragma unroll
@@ -474,12 +501,15 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
 #pragma unroll
       for (int e = 0; e < kV; ++e) x[u * kV + e] = in ? y[e] : -INFINITY;
     }
-    if (kHeld == 0 && step + 1 < steps) load(step + 1, v);
-    float top = -INFINITY;
+    if (kHeld == 0 && step + 1 < steps) load(step + 1, next);
+    float top = -INFINITY, low = INFINITY;
 #pragma unroll
-    for (int i = 0; i < kLpVecs * kV; i += 2) top = fmaxf(fmaxf(x[i], x[i + 1]), top);
+    for (int i = 0; i < kLpVecs * kV; i += 2) {
+      top = lp_max3(x[i], x[i + 1], top);
+      if (kTight) low = lp_min3(x[i], x[i + 1], low);
+    }
     held_top = top;
-    add(x, top);
+    add(x, top, low);
     if constexpr (kTop) {
       if constexpr (S::kLanes > 1) {  // over the block's four lanes: neighbours, then pairs
         static_assert(S::kLanes == 4 || S::kLanes == 1, "");
@@ -495,13 +525,24 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
     for (int i = 0; i < kHeld; ++i) {
       tops[i] = -INFINITY;
       if (i >= steps) continue;
-      if ((i + 1) * S::kStep <= w.vecs) take(i, cur[i], tops[i], std::true_type{});
-      else take(i, cur[i], tops[i], std::false_type{});
+      if ((i + 1) * S::kStep <= w.vecs) take(i, cur[i], cur[i], tops[i], std::true_type{});
+      else take(i, cur[i], cur[i], tops[i], std::false_type{});
     }
   } else {
-    for (int step = 0; step < steps; ++step) {
-      if ((step + 1) * S::kStep <= w.vecs) take(step, cur[0], tops[0], std::true_type{});
-      else take(step, cur[0], tops[0], std::false_type{});
+    const int whole = w.vecs / S::kStep;
+    int step = 0;
+    constexpr int kOther = kTight ? 1 : 0;
+    if (!kTight)
+      for (; step < whole; ++step) take(step, cur[0], cur[0], tops[0], std::true_type{});
+    for (; kTight && step + 1 < whole; step += 2) {
+      take(step, cur[0], cur[kOther], tops[0], std::true_type{});
+      take(step + 1, cur[kOther], cur[0], tops[0], std::true_type{});
+    }
+    if (kTight && step < whole) {
+      take(step, cur[0], cur[kOther], tops[0], std::true_type{});
+      if (whole < steps) take(whole, cur[kOther], cur[0], tops[0], std::false_type{});
+    } else if (whole < steps) {
+      take(whole, cur[0], cur[kOther], tops[0], std::false_type{});
     }
   }
   int edge;
@@ -514,7 +555,7 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
     if (edge >= 0) {
       x[0] = edge_z = to_f32<T>(z[edge]);
       top = fmaxf(x[0], -INFINITY);  // (not a NaN)
-      add(x, top);
+      add(x, top, x[0]);
     }
     if constexpr (kTop) {
       if (wave == 0) {
@@ -571,7 +612,7 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
           float y[kV], top = -INFINITY;
           lp_widen<T>(cur[i][u], y);
 #pragma unroll
-          for (int e = 0; e < kV; e += 2) top = fmaxf(fmaxf(y[e], y[e + 1]), top);
+          for (int e = 0; e < kV; e += 2) top = lp_max3(y[e], y[e + 1], top);
           if (vec < w.vecs && top >= at_least) {
 #pragma unroll
             for (int e = 0; e < kV; ++e) offer(y[e], w.first + vec * kV + e);
