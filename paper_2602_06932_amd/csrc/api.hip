@@ -820,7 +820,8 @@ int aurora_token_logprobs_workspace_bytes(const aurora_logprob_desc* desc, size_
   int rc = check_logprob(desc);
   if (rc != AURORA_OK) return rc;
   // few rows are cut into parts where many are not: what is enough for many is enough for any less
-  *out_bytes = std::max(plan_logprob(desc, desc->rows).bytes, plan_logprob(desc, std::min<int>(desc->rows, logprob_few_rows())).bytes);
+  const int few = std::min<int>(desc->rows, logprob_few_rows(desc->vocab, desc->dtype == AURORA_BF16));
+  *out_bytes = std::max(plan_logprob(desc, desc->rows).bytes, plan_logprob(desc, few).bytes);
   return AURORA_OK;
 }
 

@@ -12,10 +12,11 @@
 // entries that are read lie below those that are written.  Tokens of a page taken in this call find it the same way, not through
 // the table.
 //
-// Bound by latency, except where it writes a position and a slot for each of a million rows.  Up to 1024 requests every workgroup forms
-// the prefix sums itself, four requests a thread, and does its share of the writing: one launch.  Where more than one workgroup
-// is wanted and an output is the input that the others still read, or there are more requests, one workgroup plans into the workspace
-// and a second launch writes.
+// Bound by latency: a launch, the lengths, a search and one or two loads in turn - 4.0 us for 32 requests of five tokens, 5.6 for 256
+// that grow, shrink, end and begin with 112 000 rows, 7.4 for a million rows, of which writing their positions and slots is 1.6 at a
+// copy's rate.  Up to 1024 requests every workgroup forms the prefix sums itself, four requests a thread, and does its share of the
+// writing: one launch.  Where more than one workgroup is wanted and an output is the input that the others still read, or there are
+// more requests, one workgroup plans into the workspace and a second launch writes.
 #include "launch.hpp"
 
 #include <algorithm>
@@ -305,7 +306,8 @@ size_t cache_plan_work_bytes(int batch) { return 16 + 5 * ((size_t)batch + 1) * 
 hipError_t launch_cache_plan(const CachePlanLaunch& plan, hipStream_t st) {
   CachePlanLaunch P = plan;
   P.page_shift = (P.page & (P.page - 1)) == 0 ? __builtin_ctz(P.page) : -1;
-  // Few rows are given a thread each: four that belong to two or three requests are as many loads in turn.  A workgroup per 256 or 1024
+  // Few rows are given a thread each: four that belong to two or three requests are as many loads in turn (us with one and with four:
+  // 160 rows 4.0 and 6.1, 112 000 5.6 and 9.0, 2^20 9.7 and 7.5, where writes of 16 bytes count).  A workgroup per 256 or 1024
   // rows, and per 4096 cells of the table (how many cells change hands only the lengths say).
   const bool few = P.max_rows <= kPlanFewRows;
   const int64_t rows = P.slots ? ((int64_t)P.max_rows + (few ? 255 : 1023)) / (few ? 256 : 1024) : 0;

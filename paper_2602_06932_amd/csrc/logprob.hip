@@ -11,11 +11,17 @@
 // cancels.  Logits so large that x leaves fp32's range (a mask of the type's lowest value, and nothing else left) are subtracted first.
 // A row goes to one workgroup where there are many; few rows are split, and a second launch joins the parts.
 //
-// Alternatives ride in the same pass at three lane exchanges and one LDS write per 128 (16-bit: 256) elements: the maximum of every such
-// block of the row.  The n-th largest block maximum is a lower bound on the n-th largest element, and only blocks that
-// reach it are read again - n of a thousand, most often.  What they hold at or above the bound is a short list, ranked by counting.
-// A row where it is not short (long runs of equal values, a mask that leaves less than n, values that rise along the row) takes
-// bounded steps more: the exact n-th largest of the blocks above the bound, and equal values in the order of their ids.
+// Alternatives ride in the same pass at two lane exchanges and one LDS write per 64 (16-bit: 128) elements: the maximum of every such
+// block of the row, and of 64 columns of blocks.  The n-th largest column maximum is a lower bound on the n-th largest element, and
+// only blocks that reach it are read again - little more than n of a thousand, most often.  What they hold at or above the bound is a
+// short list, ranked by counting.  A row where it is not short (long runs of equal values, a mask that leaves less than n, values that
+// rise along the row) takes bounded steps more: the n-th largest block maximum, the exact n-th largest of the blocks above it, and equal
+// values in the order of their ids.
+//
+// The logits are read with loads that do not stay in the caches: 4096 x 32000 fp32 126 -> 80 us = 6.5 TB/s, what a read of memory
+// gives; 1280 x 200064 bf16 with eight alternatives 87 us = 5.9; 160 x 128256 fp32 with twenty 21 and 4 for the merge, of which the
+// read is 13 and a workgroup's selection 5, after it.  The gradient: 4096 x 32000 fp32 201 us, 1024 x 128256 bf16 100 = 5.2 TB/s, as a
+// device copy.
 #include "launch.hpp"
 
 #include <algorithm>
@@ -43,8 +49,7 @@ constexpr float kLpLog2e = 1.4426950408889634f;
 constexpr double kLpLn2 = 0.69314718055994530942;
 constexpr float kLpFloor = -1e4f;  // stands in for -inf times zero: 2^-10000 is zero as well
 // The reference only moves when a logit is so many bits above it: exponentials stay below 2^8, as exact as below 1, and the move - 60
-// instructions, of which some lane of a wavefront has need in nearly every step if every new maximum counts - becomes rare
-// (1280 x 200064 bf16: 10.7 vector instructions an element, the units 97 % busy -> 7.3).
+// instructions, of which some lane of a wavefront has need in nearly every step if every new maximum counts - becomes rare.
 constexpr float kLpLazyBits = 8.f;
 constexpr int kLpGridRows = 1 << 22;
 
@@ -429,9 +434,9 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   const int steps = (w.vecs + S::kStep - 1) / S::kStep;
   const u32x4_t* vp = (const u32x4_t*)(z + w.first);
 
-  // Two elements a word are as many instructions a byte again: 16-bit rows are bound by them (7.3 an element, the units 90 % busy), so
-  // that two buffers that need no moves, and one test a step in place of one an element, pay.  fp32 rows are slower for both (4096 x
-  // 32000 83 -> 87 us: 144 registers).
+  // Two elements a word are twice the instructions a byte: 16-bit rows are near the vector units' limit (1280 x 200064: 97 % busy with
+  // 10.7 instructions an element, 81 % now with 8.4), so that two buffers that need no moves, and one test a step in place of one
+  // an element, pay.  fp32 rows are slower for both (4096 x 32000 83 -> 87 us: 144 registers).
   constexpr bool kTight = sizeof(T) == 2;
   u32x4_t cur[kHeld > 0 ? kHeld : kTight ? 2 : 1][kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
@@ -801,15 +806,23 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
-// Workgroups per row: one where the rows fill the chip (256 compute units, several workgroups each); few rows are cut into parts that a
-// workgroup holds in registers.  And never more than a workgroup's block maxima allow.
-constexpr int kLpHeld = 4, kLpFewRows = 640;
-int logprob_splits(int64_t rows, int V, bool bf16) {
-  constexpr int64_t most = (int64_t)LpWide::kStep * LpWide::kMaxSteps, held = (int64_t)LpWide::kStep * kLpHeld;
-  const int64_t vecs = V / (bf16 ? 8 : 4), least = (vecs + most - 1) / most, want = (vecs + held - 1) / held;
-  return (int)std::max<int64_t>(rows <= kLpFewRows && want <= kLpMaxSplits ? want : least, 1);
+// Workgroups per row: one where the rows fill the chip, and never more than a workgroup's block maxima allow; few rows are cut into parts
+// that a workgroup holds in registers.  The merge's launch is the price, the more rows the longer, the gain a row's length: us whole
+// and cut, five alternatives, 128256 fp32 (eight parts) 26.3 and 19.5 at 128 rows, 34.6 and 34.0 at 320, 46.5 and 48.2 at 512; 151936 bf16
+// (five) 23.8 and 19.5 at 128, 24.5 and 26.4 at 256; 45000 fp32 (three) 12.2 and 11.3 at 80, 13.0 and 13.6 at 144; 32000 fp32 (two)
+// 8.3 and 8.7 at one row, 11.2 and 13.3 at 176.
+constexpr int kLpHeld = 4, kLpHeldRows = 640, kLpCutParts = 3, kLpRowsPerPart = 40;
+static int64_t logprob_parts(int V, bool bf16) {
+  constexpr int64_t held = (int64_t)LpWide::kStep * kLpHeld;
+  const int64_t parts = (V / (bf16 ? 8 : 4) + held - 1) / held;
+  return parts >= kLpCutParts && parts <= kLpMaxSplits ? parts : 1;
 }
-int logprob_few_rows() { return kLpFewRows; }
+int logprob_few_rows(int V, bool bf16) { return std::min((int)logprob_parts(V, bf16) * kLpRowsPerPart, kLpHeldRows); }
+int logprob_splits(int64_t rows, int V, bool bf16) {
+  constexpr int64_t most = (int64_t)LpWide::kStep * LpWide::kMaxSteps;
+  const int64_t least = (V / (bf16 ? 8 : 4) + most - 1) / most;
+  return (int)std::max<int64_t>({rows <= logprob_few_rows(V, bf16) ? logprob_parts(V, bf16) : 1, least, 1});
+}
 int logprob_max_top() { return kLpMaxTop; }
 int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kStep * 4; }
 
@@ -831,7 +844,7 @@ static hipError_t launch_logprob_t(const LogprobLaunch& P, hipStream_t st) {
     else hipLaunchKernelGGL((logprob_rows_kernel<T, S, false, HELD>), grid, dim3(S::kThreads), 0, st, P);             \
   } while (0)
   const int64_t vecs = P.V / LpType<T>::kV;
-  if ((vecs + P.splits - 1) / P.splits <= kLpHeld * LpWide::kStep && P.rows <= kLpFewRows) AURORA_LOGPROB(LpWide, kLpHeld);
+  if ((vecs + P.splits - 1) / P.splits <= kLpHeld * LpWide::kStep && P.rows <= kLpHeldRows) AURORA_LOGPROB(LpWide, kLpHeld);
   else if (P.splits == 1 && P.rows >= kLpNarrowRows && vecs <= (P.n_top > 0 ? kLpNarrowVecsTop : kLpNarrowVecs)) AURORA_LOGPROB(LpNarrow, 0);
   else AURORA_LOGPROB(LpWide, 0);
 #undef AURORA_LOGPROB

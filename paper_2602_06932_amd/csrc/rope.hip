@@ -12,6 +12,9 @@
 // reads and writes is worked out once.  The angles of a block's rows are formed once and shared through LDS while the first rows are on
 // their way: t f in 64 bits, its whole turns dropped there - at position 10^6 float32 holds an angle to a sixteenth of a radian only - and the
 // sine and cosine of what is left in 32.
+//
+// 16384 rows of 32 + 8 + 8 heads of 128, bf16: 77 us = 5.2 TB/s, what a device copy of as many bytes takes; the gradients of 8192 57 us
+// = 5.3; 8192 rows of 48 + 8 + 8 into an 8-bit cache, half of each head turned, 52 us = 4.8; 160 rows 3.8 us.
 #include "launch.hpp"
 
 #include <algorithm>
@@ -19,6 +22,9 @@
 
 namespace aurora {
 
+// The units of a row are cut into workgroups of so many, and each forms its rows' angles again.  Between small ones that do so more often
+// and large ones that wait for each other longer: 192, 128 and 256 threads take 77, 78 and 82 us for the first of these (384 units a
+// row), 57, 56 and 57 for the gradients, 52, 59 and 54 for the third (512).
 constexpr int kRopeThreads = 192;
 constexpr int kRopeAhead = 2;  // rows on their way, and of a block where there are many
 
