@@ -138,6 +138,91 @@ def test_a_server_prefills_verifies_and_rolls_back(gpu_lib, dtype, d):
     assert int(s.count) == s.P and sorted(s.free.tolist()) == list(range(s.P))
 
 
+class Loop:
+    """One step of a server with everything it needs on the GPU: nothing of it goes through the host."""
+
+    def __init__(self, av, s, nq, H, V):
+        self.av, self.s, self.nq = av, s, nq
+        B, i32 = s.B, lambda *z: torch.zeros(z, dtype=torch.int32, device="cuda")
+        f32 = lambda *z: torch.zeros(z, device="cuda")
+        self.grow = av.aurora_cache_plan_desc(batch=B, page_size=s.page, max_pages_per_seq=s.width, num_pages=s.P, max_rows=B * nq)
+        self.back = av.aurora_cache_plan_desc(batch=B, page_size=s.page, max_pages_per_seq=s.width, num_pages=s.P)
+        w = (s.hq + 2 * s.hkv) * s.d
+        self.rope = av.aurora_rope_desc(rows=B * nq, num_q_heads=s.hq, num_kv_heads=s.hkv, head_dim=s.d, rotary_dim=s.d, page_size=s.page, num_pages=s.P,
+                                        dtype=s.code, q_stride=w, k_stride=w, v_stride=w)
+        self.ad, self.cd = s.attn_desc(nq), av.aurora_accept_desc(batch=B, num_q=nq, hidden=H, vocab=V, dtype=s.code, temperature=0.0)
+        self.ld = av.aurora_logprob_desc(rows=B * nq, vocab=V, dtype=av.AURORA_F32, n_top=3)
+        self.qkv, self.hidden, self.w = (torch.zeros(z, dtype=s.dt, device="cuda") for z in ((B * nq, w), (B, nq, H), (V, H)))
+        self.tokens, self.alen, self.nxt, self.mask = i32(B, nq), i32(B), i32(B), torch.zeros(B, nq, dtype=torch.uint8, device="cuda")
+        self.lens, self.positions, self.slots = i32(B), i32(B * nq), i32(B * nq)
+        self.q, self.out = (torch.zeros(B, nq, s.hq, s.d, dtype=s.dt, device="cuda") for _ in range(2))
+        self.lp, self.ent, self.tops, self.topl = f32(B * nq), f32(B * nq), i32(B * nq, 3), f32(B * nq, 3)
+        ws = lambda n: torch.full((max(n, 1),), 0xff, dtype=torch.uint8, device="cuda")
+        self.pws, self.vws = ws(av.aurora_cache_plan_workspace_bytes(self.grow)), ws(av.aurora_verify_workspace_bytes(self.ad, self.cd))
+        self.lws = ws(av.aurora_token_logprobs_workspace_bytes(self.ld))
+
+    def run(self):
+        av, s = self.av, self.s
+        av.aurora_cache_plan(self.grow, s.lens, s.lens + self.nq, s.table, s.free, s.count, s.count, self.lens, None, self.positions, self.slots, None, self.pws)
+        q, k, v = (x.unflatten(1, (-1, s.d)) for x in self.qkv.split([s.hq * s.d, s.hkv * s.d, s.hkv * s.d], 1))
+        av.aurora_rope_append(self.rope, q, k, v, self.positions, self.slots, s.freqs, self.q, s.kp, s.vp)
+        av.aurora_verify(self.ad, self.cd, self.q, s.kp, s.vp, s.table, self.lens, None, self.out, self.hidden, self.w, self.tokens, None, None, self.alen, self.nxt,
+                         self.mask, None, None, self.vws)
+        follow = torch.cat([self.tokens[:, 1:], self.nxt[:, None]], 1).contiguous()
+        av.aurora_token_logprobs(self.ld, av.aurora_verify_logits_ptr(self.ad, self.cd, self.vws), follow, self.lp, self.ent, None, self.tops, self.topl, self.lws)
+        av.aurora_cache_plan(self.back, self.lens, self.lens - self.nq + 1 + self.alen, s.table, s.free, s.count, s.count, s.lens, None, None, None, None, self.pws)
+
+    def results(self):
+        s = self.s
+        return [s.table, s.free, s.count, s.lens, self.lens, self.slots, self.positions, self.out, self.alen, self.nxt, self.lp, self.ent, self.tops, self.topl]
+
+
+def test_a_captured_step_of_all(gpu_lib):
+    """Plan, append, verification, log probabilities and rollback in one graph, replayed: step by step what the calls give one by one."""
+    av = gpu_lib
+    B, hq, hkv, d, page, nq, H, V = 5, 8, 2, 128, 16, 5, 256, 2003
+    loops = []
+    for _ in range(2):
+        torch.manual_seed(6)
+        s = Server(av, B, hq, hkv, d, page, 8, "bf16")
+        s.plan(torch.tensor([1, 30, 16, 77, 15], dtype=torch.int32, device="cuda"), 139)
+        s.append(torch.randn(139, (hq + 2 * hkv) * d, device="cuda").to(s.dt))
+        loops.append(Loop(av, s, nq, H, V))
+        loops[-1].w.copy_(torch.randn(V, H, device="cuda") * 0.1)
+    eager, captured = loops
+    state = lambda o: [o.s.table, o.s.free, o.s.count, o.s.lens]
+    kept = [x.clone() for x in state(captured)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        captured.run()                                          # (what the first call of a process does is not captured)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured.run()
+    for x, y in zip(state(captured), kept):
+        x.copy_(y)
+    for step in range(4):
+        for name in ("qkv", "hidden"):
+            getattr(eager, name).copy_(torch.randn_like(getattr(eager, name)))
+            getattr(captured, name).copy_(getattr(eager, name))
+        eager.tokens.copy_(torch.randint(0, V, (B, nq), device="cuda"))
+        top = (eager.hidden.float().view(-1, H) @ eager.w.float().T).argmax(1).view(B, nq)
+        for b in range(B):
+            eager.tokens[b, 1:1 + (b + step) % nq] = top[b, :(b + step) % nq].to(torch.int32)
+        captured.tokens.copy_(eager.tokens)
+        torch.cuda.synchronize()
+        g.replay()
+        eager.run()
+        torch.cuda.synchronize()
+        assert eager.alen.tolist() == [(b + step) % nq for b in range(B)]
+        for x, y in zip(eager.results(), captured.results()):
+            assert torch.equal(x, y), step
+        rows = lambda o, pool: pool.view(o.s.P, hkv, page, d).transpose(1, 2).reshape(-1, hkv, d)[o.slots.long()]
+        for a, b in ((eager.s.kp, captured.s.kp), (eager.s.vp, captured.s.vp)):
+            assert torch.equal(rows(eager, a), rows(captured, b)) and torch.isfinite(rows(eager, a).float()).all()
+
+
 def test_the_gradient_of_projections_through_rotation_and_attention(gpu_lib):
     """fp32: rope -> attention -> <dout, out>, back to q, k and v, against reverse mode in float64 on the whole chain."""
     av = gpu_lib
