@@ -609,7 +609,8 @@ int aurora_rope_frequencies(const aurora_rope_scaling* scaling, double* frequenc
  * Elements between rows are left as they are.
  *
  * Exponentials in fp32, sums over a row in fp64 in a fixed order: bit-reproducible.  A logsumexp past fp32's range (a row of the lowest
- * value at T < 1) becomes infinite.  The workspace is the forward call's; one that is enough for some rows is enough for fewer.
+ * value at T < 1) becomes infinite.  The backward takes p from the float32 lse: where |lse| is large (rows of nothing but a mask's value)
+ * it is as exact as that.  Temperatures below 2^-126 count as 2^-126.  The workspace is the forward call's; one that is enough for some rows is enough for fewer.
  * AURORA_ERR_UNSUPPORTED for n_top > 32 or more than 2^24 logits a row.
  */
 typedef struct {

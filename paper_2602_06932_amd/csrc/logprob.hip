@@ -8,7 +8,7 @@
 // t = sum (x - r) e^(x - r), in units of log 2, so that H = log s - t / s takes no second pass; moving the reference by d turns (s, t)
 // into (s, t + d s) 2^d.  Sixteen or 32 elements are summed in 32 bits at a time, their sums in 64: a row may have a million
 // entries.  r is the value that was really subtracted, rounded as it is, and the outputs are formed from it, so that its rounding
-// cancels.  Logits so large that x leaves fp32's range (a mask of the type's lowest value, and nothing else left) are subtracted first.
+// cancels.  Logits so large that its rounding would not be small (a mask's value, and nothing else left) are subtracted first.
 // A row goes to one workgroup where there are many; few rows are split, and a second launch joins the parts.
 //
 // Alternatives ride in the same pass at two lane exchanges and one LDS write per 64 (16-bit: 128) elements: the maximum of every such
@@ -23,6 +23,8 @@
 // read is 13 and a workgroup's selection 5, after it.  The gradient: 4096 x 32000 fp32 201 us, 1024 x 128256 bf16 100 = 5.2 TB/s, as a
 // device copy.
 #include "launch.hpp"
+
+#include <float.h>
 
 #include <algorithm>
 #include <type_traits>
@@ -113,8 +115,9 @@ __device__ __forceinline__ LpPart lp_part(const T* row, int V, int split, int sp
   return p;
 }
 
-// what is subtracted for the reference m: its rounded multiple, or, past kLpFar / c, m itself before the product
-constexpr float kLpFar = 8.5e37f;
+// What is subtracted for the reference m: its rounded multiple, or, past kLpFar / c, m itself before the product - there the rounding
+// alone would be a sixteenth and more (at 10^10 it is 512, and every exponential zero, or infinite).  Past kLpLimit a product may overflow.
+constexpr float kLpFar = 0x1p20f, kLpLimit = 8.5e37f;
 __device__ __forceinline__ bool lp_far(float m, float c) { return fabsf(m) * c > kLpFar; }
 __device__ __forceinline__ double lp_ref(float m, float c) { return lp_far(m, c) ? (double)m * (double)c : (double)(m * c); }
 
@@ -178,7 +181,7 @@ __device__ __forceinline__ double lp_finish(const LogprobLaunch& P, size_t row, 
 
 __device__ __forceinline__ float lp_temperature(const LogprobLaunch& P, size_t row) {
   const float T = P.temperatures ? P.temperatures[row] : P.temperature;
-  return T > 0.f ? T : 1.f;
+  return T > 0.f ? fminf(fmaxf(T, FLT_MIN), FLT_MAX) : 1.f;  // (its reciprocal is finite, and not zero)
 }
 __device__ __forceinline__ float lp_scale(const LogprobLaunch& P, size_t row) { return kLpLog2e / lp_temperature(P, row); }
 
@@ -458,7 +461,7 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   LpSums mine = {-INFINITY, 0.0, 0.0};
   float col = -INFINITY;
   float neg = 0.f;  // minus the reference
-  const float lazy = kLpLazyBits / c, lowest = -kLpFar / c;
+  const float lazy = fminf(kLpLazyBits / c, FLT_MAX), lowest = -kLpLimit / c;  // (at most -inf, which `low` may be too)
   bool far = false;
   // takes elements into the running sums (top, low: the largest and the smallest).  0 times -inf must not get into t: where there is
   // one, or a value whose x would be, distances stop at the floor.
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
       for (int i = 0; i < n; ++i) x[i] -= mine.m;
       neg = 0.f;
     }
-    if (!kTight || far || low < lowest) sums(x, std::true_type{});
+    if (!kTight || far || low <= lowest) sums(x, std::true_type{});
     else sums(x, std::false_type{});
   };
 

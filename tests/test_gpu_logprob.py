@@ -204,6 +204,49 @@ def test_a_temperature_for_every_row(gpu_lib):
     _check(gpu_lib, _logits(9, 7, 3001, "f32"), _tokens(9, 7, 3001), 1.0, 7, temps=temps)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_temperatures_far_from_one(gpu_lib, dtype):
+    """Masked rows where a scaled limit of the type overflows, in all the ways a row is dealt out; logits past each other's range."""
+    for T in (5.9, 50.0, 3e4, 1e38):
+        _check(gpu_lib, _logits(31, 6, 5003, dtype, "masked"), _tokens(31, 6, 5003), T, 8)
+    for M, V in ((700, 5003), (1100, 777)):
+        _check(gpu_lib, _logits(32, M, V, dtype, "masked"), _tokens(32, M, V), 8.0, 4, grad=False)
+    z = _logits(33, 6, 5003, dtype)
+    z[:, ::3] = -float("inf")
+    _check(gpu_lib, z, _tokens(33, 6, 5003), 1e-30, 8)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_large_values(gpu_lib, dtype):
+    """Nothing left but a mask's value, of any size; or large values next to each other, whose exponents are larger than their steps."""
+    for M, n_top in ((9, 5), (660, 5)):
+        z = torch.empty(M, 1500)
+        for m in range(M):
+            z[m] = [-1e5, -1e6, -3e7, -1e9, -1e10, -1e15, -1e30, 1e10, 2e37][m % 9]
+        z[:, 7::50] = -float("inf")
+        for T in (1.0, 0.37, 5.9):
+            _check(gpu_lib, z.to(DT[dtype]), _tokens(35, M, 1500), T, n_top, grad=False)
+    z = _logits(36, 12, 1500, "f32")
+    z[:] = z.to(DT[dtype])
+    big = torch.tensor([2.0 ** e for e in (10, 16, 19, 20, 21, 22)]).repeat(2)[:, None]
+    z = (z.clamp(-3, 3) + torch.cat([big[:6], -big[6:]])).to(DT[dtype])
+    for T in (1.0, 3.0):
+        _check(gpu_lib, z, _tokens(37, 12, 1500), T, 5, grad=False)
+
+
+def test_temperatures_past_the_normal_numbers(gpu_lib):
+    """Those below 2^-126 count as that, infinity as the largest finite one."""
+    z = _logits(34, 4, 3001, "f32", "masked")
+    tok = _tokens(34, 4, 3001)
+    big = float(torch.finfo(torch.float32).max)
+    for odd, like in ((1e-42, 2.0 ** -126), (float("inf"), big)):
+        got, want = (_run(gpu_lib, z, tok, 1.0, 4, temps=torch.full((4,), T, device="cuda"))[0] for T in (odd, like))
+        for name in got:
+            assert np.array_equal(got[name], want[name]), (odd, name)
+            assert not np.isnan(got[name].astype(np.float64)).any(), (odd, name)
+    assert np.array_equal(_run(gpu_lib, z, tok, 1e-42, 4)[0]["top_logprobs"], _run(gpu_lib, z, tok, 2.0 ** -126, 4)[0]["top_logprobs"])
+
+
 def test_nan_and_infinity_reach_the_results_of_their_row_alone(gpu_lib):
     z = _logits(10, 6, 5000, "f32")
     z[1, 77], z[2, 4999], z[4] = float("nan"), float("inf"), float("nan")
