@@ -620,7 +620,8 @@ typedef struct {
   int32_t n_top;             /* alternatives a row, 0..32                                     */
   int64_t row_stride;        /* elements from row to row; 0 => vocab                          */
   float temperature;         /* T; 0 => 1                                                     */
-  const float* temperatures; /* one for every row: DEVICE float32 [rows] (0: 1, as row_lse of a greedy request), or NULL */
+  const float* temperatures; /* DEVICE float32 (0: 1, as row_lse of a greedy request), or NULL  */
+  int32_t temperature_rows;  /* consecutive rows that share one of them (a request's, say); 0 => 1 */
 } aurora_logprob_desc;
 
 int aurora_token_logprobs_workspace_bytes(const aurora_logprob_desc* desc, size_t* out_bytes);

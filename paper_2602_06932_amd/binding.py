@@ -83,7 +83,7 @@ class aurora_rope_scaling(C.Structure):
 
 class aurora_logprob_desc(C.Structure):
     _fields_ = [("rows", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("n_top", C.c_int32), ("row_stride", C.c_int64),
-                ("temperature", C.c_float), ("temperatures", C.c_void_p)]
+                ("temperature", C.c_float), ("temperatures", C.c_void_p), ("temperature_rows", C.c_int32)]
 
 
 class AuroraError(RuntimeError):

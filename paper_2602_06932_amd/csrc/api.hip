@@ -691,7 +691,7 @@ int check_logprob(const aurora_logprob_desc* d) {
   if (!d || d->rows < 0 || d->vocab < 1 || d->n_top < 0 || d->row_stride < 0 || (d->row_stride && d->row_stride < d->vocab))
     return AURORA_ERR_INVALID_ARG;
   if (d->dtype != AURORA_F32 && d->dtype != AURORA_BF16) return AURORA_ERR_INVALID_ARG;
-  if (!(d->temperature >= 0.f) || !(d->temperature < INFINITY)) return AURORA_ERR_INVALID_ARG;
+  if (!(d->temperature >= 0.f) || !(d->temperature < INFINITY) || d->temperature_rows < 0) return AURORA_ERR_INVALID_ARG;
   if (d->n_top > logprob_max_top() || d->vocab > logprob_max_vocab()) return AURORA_ERR_UNSUPPORTED;
   return AURORA_OK;
 }
@@ -713,6 +713,7 @@ LogprobLaunch logprob_launch_from(const aurora_logprob_desc* d) {
   a.row_stride = d->row_stride ? d->row_stride : d->vocab;
   a.temperature = d->temperature > 0.f ? d->temperature : 1.f;
   a.temperatures = d->temperatures;
+  a.temperature_rows = d->temperature_rows > 0 ? d->temperature_rows : 1;
   return a;
 }
 }  // namespace

@@ -196,7 +196,8 @@ struct LogprobLaunch {
   bool bf16, wide;
   int64_t row_stride;
   float temperature;
-  const float* temperatures;                               // [rows] or NULL
+  const float* temperatures;                               // one for so many rows each, or NULL
+  int temperature_rows;
   const void* logits;
   const int32_t* tokens;
   float *logprob, *entropy, *lse, *top_logprobs;

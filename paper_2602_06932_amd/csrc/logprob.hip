@@ -49,7 +49,7 @@ constexpr int kLpMaxTop = 32;
 constexpr int kLpMaxSplits = 64;
 constexpr float kLpLog2e = 1.4426950408889634f;
 constexpr double kLpLn2 = 0.69314718055994530942;
-constexpr float kLpFloor = -1e4f;  // stands in for -inf times zero: 2^-10000 is zero as well
+constexpr float kLpFloor = -256.f;  // stands in for -inf times zero: 2^-256 is zero as well (and 256 times a gradient no infinity)
 // The reference only moves when a logit is so many bits above it: exponentials stay below 2^8, as exact as below 1, and the move - 60
 // instructions, of which some lane of a wavefront has need in nearly every step if every new maximum counts - becomes rare.
 constexpr float kLpLazyBits = 8.f;
@@ -180,7 +180,7 @@ __device__ __forceinline__ double lp_finish(const LogprobLaunch& P, size_t row, 
 }
 
 __device__ __forceinline__ float lp_temperature(const LogprobLaunch& P, size_t row) {
-  const float T = P.temperatures ? P.temperatures[row] : P.temperature;
+  const float T = P.temperatures ? P.temperatures[(unsigned)row / (unsigned)P.temperature_rows] : P.temperature;
   return T > 0.f ? fminf(fmaxf(T, FLT_MIN), FLT_MAX) : 1.f;  // (its reciprocal is finite, and not zero)
 }
 __device__ __forceinline__ float lp_scale(const LogprobLaunch& P, size_t row) { return kLpLog2e / lp_temperature(P, row); }

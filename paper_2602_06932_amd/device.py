@@ -175,11 +175,9 @@ class DeviceVerify:
         w = self.w
         rows = w.batch * w.num_q
         if getattr(self, "_logprob_k", None) != (n_top, after):
-            # one temperature per token row: requests' own where they have them (a greedy request's rows at temperature 1)
-            self._row_temps = None if self.temperatures is None else self.temperatures.repeat_interleave(w.num_q)
             self.logprob_desc = B.aurora_logprob_desc(
                 rows=rows, vocab=w.vocab, dtype=B.AURORA_F32, n_top=n_top, temperature=w.temperature,
-                temperatures=None if self._row_temps is None else self._row_temps.data_ptr())
+                temperatures=None if self.temperatures is None else self.temperatures.data_ptr(), temperature_rows=w.num_q)
             self.logprob, self.entropy, self.lse = (torch.empty((w.batch, w.num_q), dtype=torch.float32, device="cuda") for _ in range(3))
             self.top_ids = torch.empty((rows, n_top), dtype=torch.int32, device="cuda") if n_top else None
             self.top_logprobs = torch.empty((rows, n_top), dtype=torch.float32, device="cuda") if n_top else None

@@ -204,6 +204,27 @@ def test_a_temperature_for_every_row(gpu_lib):
     _check(gpu_lib, _logits(9, 7, 3001, "f32"), _tokens(9, 7, 3001), 1.0, 7, temps=temps)
 
 
+@pytest.mark.parametrize("vocab", [301, 50001])
+def test_rows_that_share_a_temperature(gpu_lib, vocab):
+    """Rows in threes, the last ones a part of their three: what as many entries give."""
+    av = gpu_lib
+    M, z = 8, _logits(38, 8, vocab, "f32").cuda()
+    tok = torch.arange(M, dtype=torch.int32, device="cuda")
+    temps = torch.tensor([0.6, 0.0, 1.9], device="cuda")
+    each = temps.repeat_interleave(3)[:M].contiguous()
+    got = []
+    for t, share in ((temps, 3), (each, 0)):
+        d = av.aurora_logprob_desc(rows=M, vocab=vocab, dtype=av.AURORA_F32, n_top=4, temperatures=t.data_ptr(), temperature_rows=share)
+        lp, H, lse, tl, ti = *(torch.zeros(M, device="cuda") for _ in range(3)), torch.zeros(M, 4, device="cuda"), torch.zeros(M, 4, dtype=torch.int32, device="cuda")
+        ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+        g = torch.zeros_like(z)
+        av.aurora_token_logprobs(d, z, tok, lp, H, lse, ti, tl, ws)
+        av.aurora_token_logprobs_backward(d, z, tok, H, lse, lp, H, g)
+        got.append((lp, H, lse, ti, tl, g))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_temperatures_far_from_one(gpu_lib, dtype):
     """Masked rows where a scaled limit of the type overflows, in all the ways a row is dealt out; logits past each other's range."""
@@ -214,6 +235,7 @@ def test_temperatures_far_from_one(gpu_lib, dtype):
     z = _logits(33, 6, 5003, dtype)
     z[:, ::3] = -float("inf")
     _check(gpu_lib, z, _tokens(33, 6, 5003), 1e-30, 8)
+    _check(gpu_lib, z, _tokens(33, 6, 5003), 1e-35, 8)          # (a gradient of 10^35: times a logarithm's limit it is finite)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -274,3 +274,23 @@ def test_log_probabilities_of_a_step(gpu_lib, make):
     assert np.allclose(dv.logprob.cpu().numpy().reshape(-1), ref["logprob"], atol=4e-6)
     assert np.allclose(dv.lse.cpu().numpy(), dv.row_lse.cpu().numpy(), atol=4e-6)
     assert np.array_equal(dv.top_ids.cpu().numpy(), ref["top_ids"])
+
+
+def test_log_probabilities_of_requests_with_their_own_temperatures(gpu_lib):
+    """One temperature a request, as the step has them; a change of them in place counts for the next call."""
+    from paper_2602_06932_amd.device import DeviceVerify
+    w = gen.llama_chain(4, batch=5, len_lo=40, len_hi=300, vocab=4099, hidden_size=512)
+    w.temperatures = np.array([0.7, 0.0, 1.0, 1.3, 0.2], np.float32)
+    dv = DeviceVerify(w)
+    dv.verify()
+    for scale in (1.0, 2.0):
+        dv.temperatures.mul_(scale)
+        dv.logprobs(dv.next_token[:, None].expand(-1, w.num_q).contiguous(), n_top=2)
+        torch.cuda.synchronize()
+        temps = np.repeat(dv.temperatures.cpu().numpy().astype(np.float64), w.num_q)
+        logits = dv.logits_host().reshape(-1, w.vocab).astype(np.float64)
+        ref = token_logprobs(logits, np.repeat(dv.next_token.cpu().numpy(), w.num_q), np.where(temps > 0, temps, 1.0), 2)
+        # logits of a few units over temperatures from 0.2: the common factor's 2 x 2^-24 of up to 50, and sums below 2^-20
+        assert np.allclose(dv.logprob.cpu().numpy().reshape(-1), ref["logprob"], rtol=1e-6, atol=8e-6)
+        assert np.allclose(dv.lse.cpu().numpy().reshape(-1), ref["lse"], rtol=1e-6, atol=8e-6)
+        assert np.array_equal(dv.top_ids.cpu().numpy(), ref["top_ids"])

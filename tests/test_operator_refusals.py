@@ -108,7 +108,7 @@ def _lpb(desc={}, **kw):
 
 
 @pytest.mark.parametrize("desc,want", [(dict(rows=-1), BAD), (dict(vocab=0), BAD), (dict(dtype=2), BAD), (dict(n_top=-1), BAD), (dict(row_stride=999), BAD),
-                                       (dict(row_stride=-1), BAD), (dict(temperature=-0.5), BAD), (dict(temperature=float("nan")), BAD),
+                                       (dict(row_stride=-1), BAD), (dict(temperature_rows=-1), BAD), (dict(temperature=-0.5), BAD), (dict(temperature=float("nan")), BAD),
                                        (dict(temperature=float("inf")), BAD), (dict(n_top=33), NOT), (dict(vocab=2 ** 24 + 1), NOT)])
 def test_logprob_descriptors(desc, want):
     assert _lp(desc) == want and _lpb(desc) == want
@@ -120,7 +120,7 @@ def test_a_logprob_workspace_is_enough_for_fewer_rows():
     for dtype in (av.AURORA_F32, av.AURORA_BF16):
         for vocab in (777, 32000, 200064, 1 << 24):
             n = [av.aurora_token_logprobs_workspace_bytes(_desc(av.aurora_logprob_desc, LP, rows=r, vocab=vocab, dtype=dtype, n_top=32))
-                 for r in (0, 1, 5, 100, 640, 641, 1000, 1024, 5000, 100000)]
+                 for r in (0, 1, 5, 100, 119, 120, 121, 200, 201, 320, 321, 639, 640, 641, 1000, 1024, 5000, 100000)]
             assert n == sorted(n) and all(x % 256 == 0 and x for x in n)
 
 
