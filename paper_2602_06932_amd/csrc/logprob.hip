@@ -650,7 +650,8 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
 
 // Joins the parts of a row, one workgroup each.  The parts' lists are sorted, so with more parts than alternatives the n-th largest
 // of their heads is a bound again, and few of their keys reach it.  Bound by latency: everything is loaded at once, and one wavefront
-// joins the sums while another looks for the bound.
+// joins the sums while another looks for the bound.  (A launch of its own: were the last workgroup of a row to do it, what the others hand
+// over would have to pass between the dies' caches - 160 rows x 128256 with twenty 24 us so, 37 in one launch.)
 constexpr int kLpMergeThreads = 256;
 template <typename T>
 __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobLaunch P) {
