@@ -822,7 +822,9 @@ int aurora_token_logprobs_workspace_bytes(const aurora_logprob_desc* desc, size_
   if (rc != AURORA_OK) return rc;
   // few rows are cut into parts where many are not: what is enough for many is enough for any less
   const int few = std::min<int>(desc->rows, logprob_few_rows(desc->vocab, desc->dtype == AURORA_BF16));
-  *out_bytes = std::max(plan_logprob(desc, desc->rows).bytes, plan_logprob(desc, few).bytes);
+  size_t bytes = std::max(plan_logprob(desc, desc->rows).bytes, plan_logprob(desc, few).bytes);
+  for (int rows = std::min<int>(desc->rows, logprob_idle_rows()); rows > 0; --rows) bytes = std::max(bytes, plan_logprob(desc, rows).bytes);
+  *out_bytes = bytes;
   return AURORA_OK;
 }
 

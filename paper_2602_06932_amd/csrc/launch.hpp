@@ -209,7 +209,8 @@ struct LogprobLaunch {
   unsigned long long* keys;
 };
 int logprob_splits(int64_t rows, int V, bool bf16);
-int logprob_few_rows(int V, bool bf16);  // up to so many rows are cut into parts
+int logprob_few_rows(int V, bool bf16);  // up to so many rows are cut into a number of parts that only the row gives,
+int logprob_idle_rows();                 // and up to so many into one that depends on the rows
 int logprob_max_top();
 int logprob_max_vocab();
 hipError_t launch_logprob(const LogprobLaunch& P, hipStream_t st);

@@ -814,8 +814,12 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
 // that a workgroup holds in registers.  The merge's launch is the price, the more rows the longer, the gain a row's length: us whole
 // and cut, five alternatives, 128256 fp32 (eight parts) 26.3 and 19.5 at 128 rows, 34.6 and 34.0 at 320, 46.5 and 48.2 at 512; 151936 bf16
 // (five) 23.8 and 19.5 at 128, 24.5 and 26.4 at 256; 45000 fp32 (three) 12.2 and 11.3 at 80, 13.0 and 13.6 at 144; 32000 fp32 (two)
-// 8.3 and 8.7 at one row, 11.2 and 13.3 at 176.
+// 8.3 and 8.7 at one row, 11.2 and 13.3 at 176.  Up to 64 rows leave compute units idle even so: they are cut further, down to one step
+// a part, into up to 512 parts in all, where that makes at least eight of a row (five alternatives, parts of four steps and these: 5 x
+// 128256 fp32 9.9 and 8.5, 12 x 151936 bf16 12.4 and 9.7, 64 x 64000 fp32 11.8 and 11.1, 5 x 32000 fp32 uncut 9.1, so 8.0, where it makes
+// four of a row 5 x 32000 bf16 8.3 and 9.2; in 256 or 1024 parts 64 x 64000 11.7 and 11.6, 64 x 151936 bf16 14.4, 15.8 and 16.8).
 constexpr int kLpHeld = 4, kLpHeldRows = 640, kLpCutParts = 3, kLpRowsPerPart = 40;
+constexpr int kLpIdleRows = 64, kLpIdleParts = 8;
 static int64_t logprob_parts(int V, bool bf16) {
   constexpr int64_t held = (int64_t)LpWide::kStep * kLpHeld;
   const int64_t parts = (V / (bf16 ? 8 : 4) + held - 1) / held;
@@ -825,8 +829,12 @@ int logprob_few_rows(int V, bool bf16) { return std::min((int)logprob_parts(V, b
 int logprob_splits(int64_t rows, int V, bool bf16) {
   constexpr int64_t most = (int64_t)LpWide::kStep * LpWide::kMaxSteps;
   const int64_t least = (V / (bf16 ? 8 : 4) + most - 1) / most;
-  return (int)std::max<int64_t>({rows <= logprob_few_rows(V, bf16) ? logprob_parts(V, bf16) : 1, least, 1});
+  const int64_t steps = std::min<int64_t>((V / (bf16 ? 8 : 4) + LpWide::kStep - 1) / LpWide::kStep, kLpMaxSplits);
+  const int64_t cut = rows <= logprob_few_rows(V, bf16) ? logprob_parts(V, bf16) : 1;
+  const int64_t most_of_row = kLpIdleRows * kLpIdleParts / std::max<int64_t>(rows, 1);  // (eight or more up to 64 rows)
+  return (int)std::max<int64_t>({rows <= kLpIdleRows && steps >= kLpIdleParts ? std::min(steps, most_of_row) : 1, cut, least, 1});
 }
+int logprob_idle_rows() { return kLpIdleRows; }
 int logprob_max_top() { return kLpMaxTop; }
 int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kStep * 4; }
 

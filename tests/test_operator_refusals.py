@@ -120,7 +120,7 @@ def test_a_logprob_workspace_is_enough_for_fewer_rows():
     for dtype in (av.AURORA_F32, av.AURORA_BF16):
         for vocab in (777, 32000, 200064, 1 << 24):
             n = [av.aurora_token_logprobs_workspace_bytes(_desc(av.aurora_logprob_desc, LP, rows=r, vocab=vocab, dtype=dtype, n_top=32))
-                 for r in (0, 1, 5, 100, 119, 120, 121, 200, 201, 320, 321, 639, 640, 641, 1000, 1024, 5000, 100000)]
+                 for r in (0, 1, 5, 7, 8, 9, 16, 17, 31, 63, 64, 65, 100, 119, 120, 121, 200, 201, 320, 321, 639, 640, 641, 1000, 1024, 5000, 100000)]
             assert n == sorted(n) and all(x % 256 == 0 and x for x in n)
 
 
