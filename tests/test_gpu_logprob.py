@@ -209,6 +209,28 @@ def test_rows_apart_and_not_aligned(gpu_lib, shift, dtype):
         _check(gpu_lib, _logits(V, 9, V, dtype), _tokens(V, 9, V), 0.9, 6, stride=stride, shift=shift)
 
 
+def test_rows_past_32_bits(gpu_lib):
+    """Rows of logits 2^31 elements apart, and their gradient in place: what the same rows side by side give."""
+    av = gpu_lib
+    M, V, far = 3, 5003, 2 ** 31 + 8
+    near = _logits(12, M, V, "f32").cuda()
+    wide = torch.zeros((M - 1) * far + V, device="cuda")
+    z = wide.as_strided((M, V), (far, 1))
+    z.copy_(near)
+    tok = torch.tensor([4, 5002, 77], dtype=torch.int32, device="cuda")
+    got = []
+    for x, stride in ((z, far), (near.clone(), 0)):
+        d = av.aurora_logprob_desc(rows=M, vocab=V, dtype=av.AURORA_F32, n_top=4, row_stride=stride)
+        ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+        o = [torch.zeros(M, device="cuda") for _ in range(3)] + [torch.zeros((M, 4), dtype=torch.int32, device="cuda"), torch.zeros((M, 4), device="cuda")]
+        av.aurora_token_logprobs(d, x, tok, *o, ws)
+        av.aurora_token_logprobs_backward(d, x, tok, o[1], o[2], o[0], o[1], x)
+        got.append(o + [x.clone()])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert torch.equal(got[1][0].cpu(), got[0][0].cpu()) and not bool(wide[V:far].any()) and not bool(wide[far + V:2 * far].any())
+
+
 def test_a_temperature_for_every_row(gpu_lib):
     temps = torch.tensor([0.5, 0.0, 1.0, 2.0, 0.0, 0.1, 3.0], device="cuda")
     _check(gpu_lib, _logits(9, 7, 3001, "f32"), _tokens(9, 7, 3001), 1.0, 7, temps=temps)

@@ -156,6 +156,54 @@ def test_gradients_turn_back(gpu_lib, kw):
         assert (_host(got)[~live] == 0).all()
 
 
+@pytest.mark.parametrize("kv8", [False, True])
+def test_a_cache_and_rows_past_32_bits(gpu_lib, kv8):
+    """Pools of more than 2^32 elements, the last slots of them; rows of queries 2^31 elements apart.  And the gradients' way back."""
+    av = gpu_lib
+    rows, hq, hkv, d, page, P, far = 5, 2, 8, 128, 16, 270000, 2 ** 31 + 64
+    kp, vp = (torch.zeros((P, hkv, page, d), dtype=torch.uint8 if kv8 else torch.bfloat16, device="cuda") for _ in range(2))
+    assert kp.numel() > 2 ** 32
+    wide = torch.zeros((rows - 1) * far + hq * d, dtype=torch.bfloat16, device="cuda")
+    q = wide.as_strided((rows, hq, d), (far, d, 1))
+    q.copy_(torch.randn(rows, hq, d, device="cuda"))
+    k, v = (torch.randn(rows, hkv, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    slots = torch.tensor([P * page - 1, 3, P * page - 33, 2 ** 22 - 1, P * page // 2], dtype=torch.int32, device="cuda")
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 1000
+    f = 10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) * 2 / d)
+    one = torch.ones(hkv, device="cuda")
+    desc = av.aurora_rope_desc(rows=rows, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, rotary_dim=d, page_size=page, num_pages=P, dtype=av.AURORA_BF16,
+                               kv_fp8=int(kv8), k_scale=one.data_ptr(), v_scale=one.data_ptr(), q_stride=far, q_out_stride=far)
+    before = _host(q)
+    av.aurora_rope_append(desc, q, k, v, pos, slots, f.cuda(), q, kp, vp)          # (in place)
+    torch.cuda.synchronize()
+    page_of, off = slots.long() // page, slots.long() % page
+    p = pos.cpu().numpy()
+    ref = rope_turn(before, p, f.numpy(), d, False)
+    assert (np.abs(_host(q) - ref) <= _turn_error(before, p, f, d, False, 1.0) + STEP["bf16"] * np.abs(ref)).all()
+    if kv8:
+        assert torch.equal(vp[page_of, :, off], v.float().to(torch.float8_e4m3fn).view(torch.uint8))
+    else:
+        assert torch.equal(vp[page_of, :, off], v)
+        ref = rope_turn(_host(k), p, f.numpy(), d, False)
+        assert (np.abs(_host(kp[page_of, :, off]) - ref) <= _turn_error(_host(k), p, f, d, False, 1.0) + STEP["bf16"] * np.abs(ref)).all()
+    at = kp[page_of, :, off].clone()
+    kp[page_of, :, off] = 0                                       # nothing else was written
+    vp[page_of, :, off] = 0
+    assert all(not bool(x.any()) for pool in (kp, vp) for x in pool.split(10000))
+    if kv8:
+        return
+    del vp
+    dk = torch.zeros((P, hkv, page, d), device="cuda")
+    dk[page_of, :, off] = at.float()
+    desc.q_out_stride, desc.num_q_heads = 0, 0
+    got, gv = torch.zeros_like(k), torch.zeros_like(v)
+    av.aurora_rope_append_backward(desc, None, dk, dk, pos, slots, f.cuda(), None, got, gv)
+    torch.cuda.synchronize()
+    x = _host(at)
+    ref = rope_turn(x, p, f.numpy(), d, False, back=True)
+    assert (np.abs(_host(got) - ref) <= _turn_error(x, p, f, d, False, 1.0) + STEP["bf16"] * np.abs(ref)).all() and torch.equal(gv, at)
+
+
 def test_in_place_queries_alone_and_without_slots(gpu_lib):
     av = gpu_lib
     for fused in (False, True):
