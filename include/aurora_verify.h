@@ -533,8 +533,9 @@ int aurora_cache_plan(const aurora_cache_plan_desc* desc, const int32_t* held_le
  *   q_out [rows, Hq, D]                    the turned queries; may be q itself with the same stride
  *   k_pages, v_pages                       pools [P, Hkv, page_size, D]: turned keys, and values, at their slots
  * num_kv_heads = 0: queries alone; k, v, k_pages, v_pages are not used, slots may be NULL (every row is one) or say by a negative
- * number that a row is none.  num_q_heads = 0: keys and values alone.  kv_fp8: the pools hold OCP E4M3 codes of value / scale (nearest, ties to even, limited to the largest finite code),
- * k_scale / v_scale [Hkv] > 0 as in aurora_attn_desc.  Arithmetic in fp32, one rounding at the end.
+ * number that a row is none.  num_q_heads = 0: keys and values alone.  kv_fp8: the pools hold OCP E4M3 codes of value / scale
+ * (nearest, ties to even, limited to the largest finite code), k_scale / v_scale [Hkv] > 0 as in aurora_attn_desc.  Arithmetic in
+ * fp32, one rounding at the end.
  *
  * aurora_rope_append_backward: from the gradients of q_out and of the pools (float32, as aurora_attn_backward writes them: dq_out with
  * q_out_stride) to those of q, k and v, of type dtype, rows with q_stride, k_stride and v_stride; zero for rows that are not one.
@@ -610,7 +611,8 @@ int aurora_rope_frequencies(const aurora_rope_scaling* scaling, double* frequenc
  *
  * Exponentials in fp32, sums over a row in fp64 in a fixed order: bit-reproducible.  A logsumexp past fp32's range (a row of the lowest
  * value at T < 1) becomes infinite.  The backward takes p from the float32 lse: where |lse| is large (rows of nothing but a mask's value)
- * it is as exact as that.  Temperatures below 2^-126 count as 2^-126.  The workspace is the forward call's; one that is enough for some rows is enough for fewer.
+ * it is as exact as that.  Temperatures below 2^-126 count as 2^-126.  The workspace is the forward call's; one that is enough for
+ * some rows is enough for fewer.
  * AURORA_ERR_UNSUPPORTED for n_top > 32 or more than 2^24 logits a row.
  */
 typedef struct {
