@@ -439,8 +439,9 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
 
   // Two elements a word are twice the instructions a byte: 16-bit rows are near the vector units' limit (1280 x 200064: 97 % busy with
   // 10.7 instructions an element, 81 % now with 8.4), so that two buffers that need no moves, and one test a step in place of one
-  // an element, pay.  fp32 rows are slower for both (4096 x 32000 83 -> 87 us: 144 registers).
-  constexpr bool kTight = sizeof(T) == 2;
+  // an element, pay.  fp32 rows are slower for both (4096 x 32000 83 -> 87 us: 144 registers), and so are short rows, a wavefront each,
+  // which wait more than they work: the more of them at a time, the better (60000 x 777 bf16 50 us, 69 with 105 registers for 79).
+  constexpr bool kTight = sizeof(T) == 2 && S::kThreads > kWave;
   u32x4_t cur[kHeld > 0 ? kHeld : kTight ? 2 : 1][kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
 #pragma unroll
@@ -498,11 +499,12 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
 
   // one step's elements, the next step's already on their way; kWhole: no vector of the step lies past the part
   float tops[kHeld > 0 ? kHeld : 1];  // a held step's maximum
-  auto take = [&](int step, u32x4_t (&v)[kLpVecs], u32x4_t (&next)[kLpVecs], float& held_top, auto whole) {
+  auto take = [&](int step, u32x4_t (&v)[kLpVecs], u32x4_t (&next)[kLpVecs], float& held_top, auto whole, auto vecs) {
     constexpr bool kWhole = decltype(whole)::value;
-    float x[kLpVecs * kV];
+    constexpr int kVecs = decltype(vecs)::value;  // that the step has at most
+    float x[kVecs * kV];
 #pragma unroll
-    for (int u = 0; u < kLpVecs; ++u) {
+    for (int u = 0; u < kVecs; ++u) {
       float y[kV];
       lp_widen<T>(v[u], y);
       const bool in = kWhole || step * S::kStep + u * S::kThreads + tid < w.vecs;
@@ -512,7 +514,7 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
     if (kHeld == 0 && step + 1 < steps) load(step + 1, next);
     float top = -INFINITY, low = INFINITY;
 #pragma unroll
-    for (int i = 0; i < kLpVecs * kV; i += 2) {
+    for (int i = 0; i < kVecs * kV; i += 2) {
       top = lp_max3(x[i], x[i + 1], top);
       if (kTight) low = lp_min3(x[i], x[i + 1], low);
     }
@@ -528,29 +530,37 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
       col = fmaxf(col, top);
     }
   };
+  constexpr std::integral_constant<int, kLpVecs> all;
   if constexpr (kHeld > 0) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       tops[i] = -INFINITY;
       if (i >= steps) continue;
-      if ((i + 1) * S::kStep <= w.vecs) take(i, cur[i], cur[i], tops[i], std::true_type{});
-      else take(i, cur[i], cur[i], tops[i], std::false_type{});
+      if ((i + 1) * S::kStep <= w.vecs) take(i, cur[i], cur[i], tops[i], std::true_type{}, all);
+      else take(i, cur[i], cur[i], tops[i], std::false_type{}, all);
     }
   } else {
     const int whole = w.vecs / S::kStep;
     int step = 0;
     constexpr int kOther = kTight ? 1 : 0;
+    // A short row's last step, which may be all of it, is worked out no further than it goes (60000 x 300 fp32 42 -> 37 us).
+    auto last = [&](u32x4_t (&v)[kLpVecs]) {
+      const int rest = w.vecs - whole * S::kStep;
+      if (S::kThreads == kWave && rest <= S::kThreads) take(whole, v, v, tops[0], std::false_type{}, std::integral_constant<int, 1>{});
+      else if (S::kThreads == kWave && rest <= 2 * S::kThreads) take(whole, v, v, tops[0], std::false_type{}, std::integral_constant<int, 2>{});
+      else take(whole, v, v, tops[0], std::false_type{}, all);
+    };
     if (!kTight)
-      for (; step < whole; ++step) take(step, cur[0], cur[0], tops[0], std::true_type{});
+      for (; step < whole; ++step) take(step, cur[0], cur[0], tops[0], std::true_type{}, all);
     for (; kTight && step + 1 < whole; step += 2) {
-      take(step, cur[0], cur[kOther], tops[0], std::true_type{});
-      take(step + 1, cur[kOther], cur[0], tops[0], std::true_type{});
+      take(step, cur[0], cur[kOther], tops[0], std::true_type{}, all);
+      take(step + 1, cur[kOther], cur[0], tops[0], std::true_type{}, all);
     }
     if (kTight && step < whole) {
-      take(step, cur[0], cur[kOther], tops[0], std::true_type{});
-      if (whole < steps) take(whole, cur[kOther], cur[0], tops[0], std::false_type{});
+      take(step, cur[0], cur[kOther], tops[0], std::true_type{}, all);
+      if (whole < steps) last(cur[kOther]);
     } else if (whole < steps) {
-      take(whole, cur[0], cur[kOther], tops[0], std::false_type{});
+      last(cur[0]);
     }
   }
   int edge;
@@ -839,8 +849,8 @@ int logprob_max_top() { return kLpMaxTop; }
 int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kStep * 4; }
 
 // Rows of so few vectors go to a wavefront each where there are many: what a row costs besides its bytes is barriers, the more of them with
-// a selection.  us with 256 threads a row and with 64: 60000 rows x 777 fp32 136 and 51, with one alternative 399 and 117; 20000 x 2048 53
-// and 31, with five 141 and 52; 10000 x 16001 bf16 with five 114 and 75; 10000 x 8192 fp32 without 53 and 55.
+// a selection.  us with 256 threads a row and with 64: 60000 rows x 777 fp32 135 and 47, with one alternative 270 and 98; 20000 x 2048 50
+// and 29, with five 96 and 43; 10000 x 16001 bf16 with five 96 and 76; 10000 x 8192 fp32 without 53 and 53.
 constexpr int kLpNarrowVecs = 1024, kLpNarrowVecsTop = 4096, kLpNarrowRows = 1024;
 static_assert(kLpNarrowVecsTop <= LpNarrow::kStep * LpNarrow::kMaxSteps, "a row's block maxima");
 
