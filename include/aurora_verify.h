@@ -600,7 +600,9 @@ int aurora_rope_frequencies(const aurora_rope_scaling* scaling, double* frequenc
  * tokens[m] outside 0 .. vocab - 1 (-1, say): the row has no token; logprob 0, no gradient from it.  -inf logits are ordinary smallest
  * values with probability 0.  A row of nothing else has lse -inf, entropy 0, log probabilities -inf and no gradient.  NaN and +inf make
  * the row's lse, entropy and log probabilities NaN; its alternatives are then unspecified (valid ids or -1).
- * tokens and logprob come as a pair; any of logprob, entropy, lse may be NULL, top_ids / top_logprobs iff n_top = 0.
+ * tokens and logprob come as a pair; any of logprob, entropy, lse may be NULL, top_ids / top_logprobs iff n_top = 0.  With lse and
+ * without alternatives a gradient is expected to follow, and the logits are read so that they stay in the caches for it, to 768 MB of them:
+ * where none does, leave lse out (up to a tenth faster).
  *
  * aurora_token_logprobs_backward: dlogits of type dtype, rows row_stride apart, from dlogprob and dentropy [rows] (either may be NULL: zero)
  *

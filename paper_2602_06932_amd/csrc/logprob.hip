@@ -18,8 +18,8 @@
 // rise along the row) takes bounded steps more: the n-th largest block maximum, the exact n-th largest of the blocks above it, and equal
 // values in the order of their ids.
 //
-// The logits are read with loads that do not stay in the caches: 4096 x 32000 fp32 126 -> 80 us = 6.5 TB/s, what a read of memory
-// gives; 1280 x 200064 bf16 with eight alternatives 87 us = 5.9; 160 x 128256 fp32 with twenty 21 and 4 for the merge: from 128 to
+// The logits are read with loads that do not stay in the caches, unless a gradient is likely to follow (kLpKeepBytes): 4096 x 32000 fp32
+// 126 -> 80 us = 6.5 TB/s, what a read of memory gives; 1280 x 200064 bf16 with eight alternatives 87 us = 5.9; 160 x 128256 fp32 with twenty 21 and 4 for the merge: from 128 to
 // 320 rows 0.085 us a row = 6.0 TB/s, and 10 us of launches, first loads, selection and merge.  The gradient: 4096 x 32000 fp32 201 us,
 // 1024 x 128256 bf16 100 = 5.2 TB/s, as a device copy.
 #include "launch.hpp"
@@ -70,6 +70,13 @@ __device__ __forceinline__ float lp_min3(float a, float b, float c) {
   float r;
   asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
+}
+
+// 16 bytes that are needed once (past the caches), or soon again
+template <bool kKeep>
+__device__ __forceinline__ u32x4_t lp_load(const u32x4_t* p) {
+  if constexpr (kKeep) return *p;
+  else return __builtin_nontemporal_load(p);
 }
 
 template <typename T> struct LpType { static constexpr int kV = 16 / (int)sizeof(T); };
@@ -420,7 +427,7 @@ __device__ __forceinline__ void lp_select(const T* row, const LpPart& w, int ste
 // ---- forward --------------------------------------------------------------------------------------------------------------
 // kHeld: the part is at most so many steps long (P.splits sees to that): all of it is on its way at once and stays in registers, so
 // that a selection reads nothing again.  0: a step at a time, the next one on its way.
-template <typename T, typename S, bool kTop, int kHeld>
+template <typename T, typename S, bool kTop, int kHeld, bool kKeep>
 __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch P) {
   constexpr int kV = LpType<T>::kV;
   __shared__ LpSums s_part[S::kWaves];
@@ -445,7 +452,7 @@ __global__ __launch_bounds__(S::kThreads) void logprob_rows_kernel(LogprobLaunch
   u32x4_t cur[kHeld > 0 ? kHeld : kTight ? 2 : 1][kLpVecs];
   auto load = [&](int step, u32x4_t (&v)[kLpVecs]) {
 #pragma unroll
-    for (int u = 0; u < kLpVecs; ++u) v[u] = __builtin_nontemporal_load(vp + min(step * S::kStep + u * S::kThreads + tid, w.vecs - 1));
+    for (int u = 0; u < kLpVecs; ++u) v[u] = lp_load<kKeep>(vp + min(step * S::kStep + u * S::kThreads + tid, w.vecs - 1));
   };
   if constexpr (kHeld > 0) {
 #pragma unroll
@@ -747,7 +754,7 @@ __global__ __launch_bounds__(kLpMergeThreads) void logprob_merge_kernel(LogprobL
 // ---- backward: elementwise, one read and one write ----------------------------------------------------------------------
 constexpr int kLpBackThreads = 256;
 constexpr int kLpBackVecs = 4;
-template <typename T>
+template <typename T, bool kKeep>
 __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(LogprobLaunch P) {
   constexpr int kV = LpType<T>::kV;
   const int tid = threadIdx.x;
@@ -777,7 +784,7 @@ __global__ __launch_bounds__(kLpBackThreads) void logprob_backward_kernel(Logpro
   for (int v0 = 0; v0 < w.vecs; v0 += kLpBackThreads * kLpBackVecs) {
     u32x4_t raw[kLpBackVecs];
 #pragma unroll
-    for (int u = 0; u < kLpBackVecs; ++u) raw[u] = __builtin_nontemporal_load(vp + min(v0 + u * kLpBackThreads + tid, w.vecs - 1));
+    for (int u = 0; u < kLpBackVecs; ++u) raw[u] = lp_load<kKeep>(vp + min(v0 + u * kLpBackThreads + tid, w.vecs - 1));
 #pragma unroll
     for (int u = 0; u < kLpBackVecs; ++u) {
       const int vec = v0 + u * kLpBackThreads + tid;
@@ -854,6 +861,13 @@ int logprob_max_vocab() { return kLpMaxSplits * LpWide::kMaxSteps * LpWide::kSte
 constexpr int kLpNarrowVecs = 1024, kLpNarrowVecsTop = 4096, kLpNarrowRows = 1024;
 static_assert(kLpNarrowVecsTop <= LpNarrow::kStep * LpNarrow::kMaxSteps, "a row's block maxima");
 
+// Up to so many bytes of logits are read so that they stay in the caches where a gradient is likely to follow: its logsumexp is wanted,
+// and no alternatives.  us, past the caches and so, forward alone and with the gradient: 134 x 32000 fp32 8.2 and 7.0, 20.8 and 18.4;
+// 1000 x 32000 22.7 and 25.6, 74.9 and 65.5; 4096 x 32000 80 and 91, 281 and 266; 1024 x 128256 bf16 49 and 54, 146 and 133; from 1 GB on
+// nothing is left of the gain (8192 x 32000 fp32 156 and 177, 554 and 553).  The gradient itself reads up to kLpKeepBackBytes so (after
+// such a forward, 134 x 32000 18.4 and 16.4, 1000 x 32000 bf16 36.1 and 36.7, fp32 65.5 and 67).
+constexpr int64_t kLpKeepBytes = (int64_t)768 << 20, kLpKeepBackBytes = (int64_t)48 << 20;
+
 static dim3 logprob_grid(int64_t n) {
   return dim3((unsigned)std::min<int64_t>(n, kLpGridRows), (unsigned)((n + kLpGridRows - 1) / kLpGridRows));
 }
@@ -862,10 +876,12 @@ static hipError_t launch_logprob_t(const LogprobLaunch& P, hipStream_t st) {
   const dim3 grid = logprob_grid((int64_t)P.rows * P.splits);
 #define AURORA_LOGPROB(S, HELD)                                                                                        \
   do {                                                                                                                \
-    if (P.n_top > 0) hipLaunchKernelGGL((logprob_rows_kernel<T, S, true, HELD>), grid, dim3(S::kThreads), 0, st, P);  \
-    else hipLaunchKernelGGL((logprob_rows_kernel<T, S, false, HELD>), grid, dim3(S::kThreads), 0, st, P);             \
+    if (P.n_top > 0) hipLaunchKernelGGL((logprob_rows_kernel<T, S, true, HELD, false>), grid, dim3(S::kThreads), 0, st, P);  \
+    else if (keep) hipLaunchKernelGGL((logprob_rows_kernel<T, S, false, HELD, true>), grid, dim3(S::kThreads), 0, st, P);    \
+    else hipLaunchKernelGGL((logprob_rows_kernel<T, S, false, HELD, false>), grid, dim3(S::kThreads), 0, st, P);             \
   } while (0)
   const int64_t vecs = P.V / LpType<T>::kV;
+  const bool keep = P.lse && (int64_t)P.rows * P.V * (int64_t)sizeof(T) <= kLpKeepBytes;
   if ((vecs + P.splits - 1) / P.splits <= kLpHeld * LpWide::kStep && P.rows <= kLpHeldRows) AURORA_LOGPROB(LpWide, kLpHeld);
   else if (P.splits == 1 && P.rows >= kLpNarrowRows && vecs <= (P.n_top > 0 ? kLpNarrowVecsTop : kLpNarrowVecs)) AURORA_LOGPROB(LpNarrow, 0);
   else AURORA_LOGPROB(LpWide, 0);
@@ -885,8 +901,11 @@ hipError_t launch_logprob_backward(const LogprobLaunch& P0, hipStream_t st) {
   P.wide = (((uintptr_t)P.grad ^ (uintptr_t)P.logits) & 15) == 0;
   P.splits = (int)std::max<int64_t>(1, std::min<int64_t>((vecs + 4095) / 4096, 4096));
   const dim3 grid = logprob_grid((int64_t)P.rows * P.splits);
-  if (P.bf16) hipLaunchKernelGGL(logprob_backward_kernel<bf16_t>, grid, dim3(kLpBackThreads), 0, st, P);
-  else hipLaunchKernelGGL(logprob_backward_kernel<float>, grid, dim3(kLpBackThreads), 0, st, P);
+  const bool keep = (int64_t)P.rows * P.V * (P.bf16 ? 2 : 4) <= kLpKeepBackBytes;
+  if (P.bf16 && keep) hipLaunchKernelGGL((logprob_backward_kernel<bf16_t, true>), grid, dim3(kLpBackThreads), 0, st, P);
+  else if (P.bf16) hipLaunchKernelGGL((logprob_backward_kernel<bf16_t, false>), grid, dim3(kLpBackThreads), 0, st, P);
+  else if (keep) hipLaunchKernelGGL((logprob_backward_kernel<float, true>), grid, dim3(kLpBackThreads), 0, st, P);
+  else hipLaunchKernelGGL((logprob_backward_kernel<float, false>), grid, dim3(kLpBackThreads), 0, st, P);
   return hipGetLastError();
 }
 

@@ -209,6 +209,34 @@ def test_rows_apart_and_not_aligned(gpu_lib, shift, dtype):
         _check(gpu_lib, _logits(V, 9, V, dtype), _tokens(V, 9, V), 0.9, 6, stride=stride, shift=shift)
 
 
+@pytest.mark.parametrize("dtype,M", [("f32", 700), ("bf16", 1400)])
+def test_large_calls_and_calls_that_leave_results_out(gpu_lib, dtype, M):
+    """Logits that are read past the caches and ones that are not: equal bits, forward with and without lse, back whole and in pieces."""
+    av = gpu_lib
+    V, step = 20003, 100
+    z = _logits(39, M, V, dtype).cuda()
+    tok = torch.from_numpy(_tokens(39, M, V).astype(np.int32)).cuda()
+    code = av.AURORA_F32 if dtype == "f32" else av.AURORA_BF16
+    new = lambda: torch.full((M,), float("nan"), device="cuda")
+    lp, H, lse, lp2, H2 = (new() for _ in range(5))
+    d = av.aurora_logprob_desc(rows=M, vocab=V, dtype=code)
+    ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+    av.aurora_token_logprobs(d, z, tok, lp, H, lse, None, None, ws)
+    av.aurora_token_logprobs(d, z, tok, lp2, H2, None, None, None, ws)
+    g, pieces = torch.zeros_like(z), torch.zeros_like(z)
+    av.aurora_token_logprobs_backward(d, z, tok, H, lse, lp, H, g)
+    for o in range(0, M, step):
+        s = slice(o, o + step)
+        av.aurora_token_logprobs_backward(av.aurora_logprob_desc(rows=step, vocab=V, dtype=code), z[s], tok[s], H[s], lse[s], lp[s], H[s], pieces[s])
+    torch.cuda.synchronize()
+    assert torch.equal(lp, lp2) and torch.equal(H, H2) and torch.equal(g, pieces)
+    # fp32: a log probability of about -13, its sums off by 2^-20 at most
+    ref = torch.log_softmax(z.double(), -1)
+    known = (tok >= 0) & (tok < V)
+    want = ref.gather(1, tok.clamp(0, V - 1).long()[:, None])[:, 0] * known
+    assert (lp - want).abs().max() < 8e-6 and (H + (ref.exp() * ref).sum(1)).abs().max() < 8e-6
+
+
 def test_rows_past_32_bits(gpu_lib):
     """Rows of logits 2^31 elements apart, and their gradient in place: what the same rows side by side give."""
     av = gpu_lib
