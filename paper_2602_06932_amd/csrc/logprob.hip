@@ -20,8 +20,8 @@
 //
 // The logits are read with loads that do not stay in the caches, unless a gradient is likely to follow (kLpKeepBytes): 4096 x 32000 fp32
 // 126 -> 80 us = 6.5 TB/s, what a read of memory gives; 1280 x 200064 bf16 with eight alternatives 87 us = 5.9; 160 x 128256 fp32 with twenty 21 and 4 for the merge: from 128 to
-// 320 rows 0.085 us a row = 6.0 TB/s, and 10 us of launches, first loads, selection and merge.  The gradient: 4096 x 32000 fp32 201 us,
-// 1024 x 128256 bf16 100 = 5.2 TB/s, as a device copy.
+// 320 rows 0.085 us a row = 6.0 TB/s, and 10 us of launches, first loads, selection and merge.  The gradient: 4096 x 32000 fp32 201 us
+// (171 after a forward that left logits in the caches), 1024 x 128256 bf16 100 = 5.2 TB/s, as a device copy.
 #include "launch.hpp"
 
 #include <float.h>
