@@ -215,7 +215,7 @@ def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
     s, n = t.stride(), t.shape
     if stride == n[-1] and t.is_contiguous():  # rows over all dimensions but the last
         return t.data_ptr()
-    if len(s) != 3 or s[0] != stride or s[2] != 1 or s[1] != n[2]:  # (not simply a view of a fused projection's output)
+    if stride == 0 or len(s) != 3 or s[0] != stride or s[2] != 1 or s[1] != n[2]:  # (not simply a view of a fused projection's output)
         dense = 1
         for k in range(len(n) - 1, 0, -1):
             if s[k] != dense and n[k] > 1:

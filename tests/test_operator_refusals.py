@@ -92,6 +92,28 @@ def test_rows_that_do_not_lie_as_the_descriptor_says():
         av.aurora_rope_append(d, x[:, 0:512:2], P, P, P, P, P, P, P, P, stream=0, check=False)
 
 
+def test_rows_that_are_one_row_expanded():
+    """Rows 0 elements apart have the storage of one: the calls would go through as many."""
+    one = torch.zeros(1, 8, 64, dtype=torch.bfloat16).expand(160, 8, 64)
+    d = _desc(av.aurora_rope_desc, ROPE, rows=160)
+    small = one[:, :2]
+    for name, t in (("q", one), ("k", small), ("v", small), ("q_out", one)):
+        a = {**ROPE_ARGS, name: t}
+        with pytest.raises(ValueError):
+            av.aurora_rope_append(d, *a.values(), stream=0, check=False)
+        with pytest.raises(ValueError):
+            av.aurora_rope_append_backward(d, a["q_out"], a["kp"], a["vp"], a["positions"], a["slots"], a["frequencies"], a["q"], a["k"], a["v"],
+                                           stream=0, check=False)
+    z = torch.zeros(1, 5, 1000).expand(4, 5, 1000)
+    with pytest.raises(ValueError):
+        _lp(dict(rows=20), logits=z)
+    for name in ("logits", "dlogits"):
+        with pytest.raises(ValueError):
+            _lpb(dict(rows=20), **{name: z})
+    for stride in (0, 700):  # a dimension of one is no such tensor, whatever its stride says
+        assert _rope(dict(rows=0, q_stride=stride), q=one[:1]) == av.AURORA_OK
+
+
 LP = dict(rows=4, vocab=1000, dtype=av.AURORA_F32, n_top=3)
 
 
