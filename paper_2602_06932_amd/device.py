@@ -170,10 +170,18 @@ class DeviceVerify:
         return st
 
     def logprobs(self, tokens, n_top=0, after="verify", stream=None):
-        """Log probabilities of `tokens` (int32 device tensor [B, Nq], -1 where there is none; the step's next_token or y_out, say),
-        entropies and the n_top largest alternatives at the step's temperature, from the logits that the last verify / accept call left."""
+        """Log probabilities of `tokens` (int32 device tensor [B, Nq], a token a row and -1 where there is none: trace()'s y_out, say, or
+        next_token[:, None].expand(-1, Nq).contiguous()), entropies and the n_top largest alternatives at the step's temperature, from the
+        logits that the last verify / accept call left."""
         w = self.w
         rows = w.batch * w.num_q
+        if isinstance(tokens, torch.Tensor):  # (or a raw address)
+            if tokens.numel() != rows:
+                raise ValueError(f"tokens: {tokens.numel()} entries, the step has {rows} rows")
+            if tokens.dtype != torch.int32:
+                raise ValueError(f"tokens: {tokens.dtype} where int32 is needed")
+            if not tokens.is_cuda:
+                raise ValueError(f"tokens: on {tokens.device}, not on the device")
         if getattr(self, "_logprob_k", None) != (n_top, after):
             self.logprob_desc = B.aurora_logprob_desc(
                 rows=rows, vocab=w.vocab, dtype=B.AURORA_F32, n_top=n_top, temperature=w.temperature,

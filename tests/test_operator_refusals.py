@@ -159,3 +159,24 @@ def test_logprob_arguments():
     assert _lpb(tokens=None) == BAD and _lpb(entropy=None) == BAD
     for name in ("logits", "tokens", "entropy", "lse", "dlogprob", "dentropy", "dlogits"):
         assert _lpb(**{name: P + 2}) == BAD, name
+
+
+def _device_verify(B=4, Nq=5, vocab=1000):
+    """A DeviceVerify with what logprobs() looks at before anything is enqueued, and without a device."""
+    from types import SimpleNamespace
+
+    from paper_2602_06932_amd.device import DeviceVerify
+    dv = object.__new__(DeviceVerify)
+    dv.w = SimpleNamespace(batch=B, num_q=Nq, vocab=vocab, temperature=1.0)
+    dv.temperatures = None
+    return dv
+
+
+def test_tokens_that_are_not_one_a_row():
+    """The step's next_token has one entry a request, not one a row: the call would read past it."""
+    on = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device="meta")
+    for tokens, why in ((on(4), "4 entries"), (on(4, 1), "4 entries"), (on(4, 4), "16 entries"), (on(4, 6), "24 entries"), (on(0), "0 entries"),
+                        (on(4, 5, dtype=torch.int64), "int64"), (on(20, dtype=torch.float32), "float32"),
+                        (torch.zeros(4, 5, dtype=torch.int32), "device")):
+        with pytest.raises(ValueError, match="tokens: .*" + why):
+            _device_verify().logprobs(tokens)
