@@ -172,7 +172,8 @@ class DeviceVerify:
     def logprobs(self, tokens, n_top=0, after="verify", stream=None):
         """Log probabilities of `tokens` (int32 device tensor [B, Nq], a token a row and -1 where there is none: trace()'s y_out, say, or
         next_token[:, None].expand(-1, Nq).contiguous()), entropies and the n_top largest alternatives at the step's temperature, from the
-        logits that the last verify / accept call left."""
+        logits that the last verify / accept call left.  The results are in logprob, entropy, lse, top_ids and top_logprobs, those of
+        calls with another n_top or `after` in buffers of their own."""
         w = self.w
         rows = w.batch * w.num_q
         if isinstance(tokens, torch.Tensor):  # (or a raw address)
@@ -182,19 +183,21 @@ class DeviceVerify:
                 raise ValueError(f"tokens: {tokens.dtype} where int32 is needed")
             if not tokens.is_cuda:
                 raise ValueError(f"tokens: on {tokens.device}, not on the device")
-        if getattr(self, "_logprob_k", None) != (n_top, after):
-            self.logprob_desc = B.aurora_logprob_desc(
+        # one set of buffers for each, kept: a captured call goes on writing to those that it was captured with
+        sets, key = self.__dict__.setdefault("_logprob_sets", {}), (n_top, after == "verify")
+        if key not in sets:
+            f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device="cuda")
+            desc = B.aurora_logprob_desc(
                 rows=rows, vocab=w.vocab, dtype=B.AURORA_F32, n_top=n_top, temperature=w.temperature,
                 temperatures=None if self.temperatures is None else self.temperatures.data_ptr(), temperature_rows=w.num_q)
-            self.logprob, self.entropy, self.lse = (torch.empty((w.batch, w.num_q), dtype=torch.float32, device="cuda") for _ in range(3))
-            self.top_ids = torch.empty((rows, n_top), dtype=torch.int32, device="cuda") if n_top else None
-            self.top_logprobs = torch.empty((rows, n_top), dtype=torch.float32, device="cuda") if n_top else None
-            self._logprob_ws = torch.empty(B.aurora_token_logprobs_workspace_bytes(self.logprob_desc), dtype=torch.uint8, device="cuda")
-            self._logprob_logits = B.aurora_verify_logits_ptr(self.attn_desc if after == "verify" else None, self.accept_desc,
-                                                              self.workspace)
-            self._logprob_k = (n_top, after)
-        return B.aurora_token_logprobs(self.logprob_desc, self._logprob_logits, tokens, self.logprob, self.entropy, self.lse,
-                                       self.top_ids, self.top_logprobs, self._logprob_ws, stream)
+            ws = torch.empty(B.aurora_token_logprobs_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+            logits = B.aurora_verify_logits_ptr(self.attn_desc if key[1] else None, self.accept_desc, self.workspace)
+            sets[key] = (desc, f32(w.batch, w.num_q), f32(w.batch, w.num_q), f32(w.batch, w.num_q),
+                         torch.empty((rows, n_top), dtype=torch.int32, device="cuda") if n_top else None,
+                         f32(rows, n_top) if n_top else None, logits, ws)
+        self.logprob_desc, self.logprob, self.entropy, self.lse, self.top_ids, self.top_logprobs, logits, ws = sets[key]
+        return B.aurora_token_logprobs(self.logprob_desc, logits, tokens, self.logprob, self.entropy, self.lse, self.top_ids,
+                                       self.top_logprobs, ws, stream)
 
     def attn_via_binding(self, stream=None):
         return B.aurora_verify_attn(self.attn_desc, self.q, self.k_pages, self.v_pages, self.block_table,

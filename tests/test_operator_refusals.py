@@ -180,3 +180,22 @@ def test_tokens_that_are_not_one_a_row():
                         (torch.zeros(4, 5, dtype=torch.int32), "device")):
         with pytest.raises(ValueError, match="tokens: .*" + why):
             _device_verify().logprobs(tokens)
+
+
+def test_a_change_of_the_alternatives_leaves_the_buffers_of_other_calls(monkeypatch):
+    """A captured call goes on writing to the buffers that it was captured with: they are there again, and not given to others in between."""
+    empty, calls = torch.empty, []
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: empty(*a, **k))
+    monkeypatch.setattr(av.binding, "aurora_verify_logits_ptr", lambda attn, accept, workspace: P if attn is None else 2 * P)
+    monkeypatch.setattr(av.binding, "aurora_token_logprobs", lambda *a: calls.append(a))
+    dv = _device_verify(B=1, vocab=128256)
+    dv.attn_desc = dv.accept_desc = dv.workspace = 0
+    for n_top, after in ((5, "verify"), (0, "verify"), (5, "accept"), (5, "verify"), (0, "verify"), (5, "accept")):
+        dv.logprobs(P, n_top, after)
+        mine = (dv.logprob_desc, 2 * P if after == "verify" else P, P, dv.logprob, dv.entropy, dv.lse, dv.top_ids, dv.top_logprobs)
+        assert all(x is y or x == y for x, y in zip(calls[-1], mine)) and (dv.top_ids is None) == (n_top == 0)  # (the last call's are the results)
+    buffers = [[x for x in c if isinstance(x, torch.Tensor)] for c in calls]
+    for a, b in zip(buffers[:3], buffers[3:]):
+        assert len(a) == len(b) and all(x is y for x, y in zip(a, b))
+    first = [x for b in buffers[:3] for x in b]
+    assert len({x.data_ptr() for x in first}) == len(first)
