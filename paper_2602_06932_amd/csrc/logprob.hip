@@ -180,7 +180,7 @@ __device__ __forceinline__ double lp_finish(const LogprobLaunch& P, size_t row, 
   if (P.entropy) P.entropy[row] = none ? 0.f : (float)(kLpLn2 * (l2 - x.t / x.s));
   if (P.logprob) {
     float lp = 0.f;
-    if (known) lp = none || z_t == -INFINITY ? -INFINITY : (float)(kLpLn2 * ((double)z_t * (double)c - r - l2));
+    if (known) lp = none ? -INFINITY : (float)(kLpLn2 * ((double)z_t * (double)c - r - l2));  // (a masked token's -inf, or the row's NaN)
     P.logprob[row] = lp;
   }
   return r + l2;

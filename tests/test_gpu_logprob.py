@@ -407,3 +407,23 @@ def test_two_graphs_and_a_stream_of_its_own(gpu_lib):
         for x, y, r in zip(a, b, ref):
             assert torch.equal(x, r) and torch.equal(y, r)
         assert torch.equal(gg, g)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V", [(6, 300), (6, 5000), (6, 70001), (700, 5000), (1100, 777)])
+def test_a_masked_token_does_not_hide_what_is_not_a_number(gpu_lib, M, V, dtype):
+    """NaN or +inf somewhere in the row and the token at -inf, in all the ways a row is dealt out; beside rows where -inf is right."""
+    z = _logits(50, M, V, dtype)
+    tok = np.random.default_rng(50).integers(0, V, M)
+    z[torch.arange(M), torch.from_numpy(tok)] = -float("inf")
+    z[0, (tok[0] + 1) % V], z[1, (tok[1] + V // 2) % V], z[2, (tok[2] - 1) % V] = float("nan"), float("inf"), float("nan")
+    z[4] = -float("inf")
+    z[5, :] = -float("inf")
+    z[5, (tok[5] + 1) % V] = float("nan")                   # nothing else left
+    for T, n_top in ((1.0, 0), (0.7, 3)):
+        got, _ = _run(gpu_lib, z, tok, T, n_top)
+        for k in ("lse", "entropy", "logprob"):
+            assert np.isnan(got[k][[0, 1, 2, 5]]).all(), k
+        rest = [m for m in range(M) if m not in (0, 1, 2, 5)]
+        assert np.isneginf(got["logprob"][rest]).all()
+        assert not np.isnan(got["lse"][rest]).any() and not np.isnan(got["entropy"][rest]).any()
