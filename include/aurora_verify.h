@@ -612,9 +612,10 @@ int aurora_rope_frequencies(const aurora_rope_scaling* scaling, double* frequenc
  * Elements between rows are left as they are.
  *
  * Exponentials in fp32, sums over a row in fp64 in a fixed order: bit-reproducible.  A logsumexp past fp32's range (a row of the lowest
- * value at T < 1) becomes infinite.  The backward takes p from the float32 lse: where |lse| is large (rows of nothing but a mask's value)
- * it is as exact as that.  Temperatures below 2^-126 count as 2^-126.  The workspace is the forward call's; one that is enough for
- * some rows is enough for fewer.
+ * value at T < 1) becomes infinite.  The backward takes p from the float32 lse: with x and lse of size s the p of a whole row are off by up
+ * to 2^-22 s, relative, whatever makes s large - an offset that the logits share, a low temperature, a mask's value and nothing else
+ * (s = 1000: 2.4e-4; from 2^22 on such a p says at most which entry is the largest).  Temperatures below 2^-126 count as 2^-126.  The
+ * workspace is the forward call's; one that is enough for some rows is enough for fewer.
  * AURORA_ERR_UNSUPPORTED for n_top > 32 or more than 2^24 logits a row.
  */
 typedef struct {

@@ -427,3 +427,74 @@ def test_a_masked_token_does_not_hide_what_is_not_a_number(gpu_lib, M, V, dtype)
         rest = [m for m in range(M) if m not in (0, 1, 2, 5)]
         assert np.isneginf(got["logprob"][rest]).all()
         assert not np.isnan(got["lse"][rest]).any() and not np.isnan(got["entropy"][rest]).any()
+
+
+def _check_gradient(av, z, tokens, T, seed, exact=True):
+    """The gradient alone, against the formula twice.  With the lse and entropy that the call is given, L and H, and i = fp32(1 / T):
+      l = x i - L is one fused product, off by u |l|, and held between -256 and 0; l log2 e is off by 2u |l| more, the exponential by 2u:
+      p = e^l is off by u (3 |l| + 3), relative, and by 2^-126 where it is less than that; g_l i, g_H i and the sum with H by 4u:
+      dz off by p i (|g_l + g_H (l + H)| u (3 |l| + 6) + |g_H| u |l| + 4u (|g_l| + |g_H| (|l| + H))), and half a step of the result.
+    And with exact ones: the given lse is off by u |lse|, the common factor's 2u max|x| and the sums' e (see above), x i by u |x|, so that l
+    is off by
+      y = u (2 max|x| + 2 |lse| + |x| + 16) + sum p e,   p by e^y - 1, relative, and log p + H by y and by what H is off."""
+    M, V = z.shape
+    T = float(np.float32(T))
+    print(f"[case] gradient {M} x {V} {z.dtype} T={T}", flush=True)
+    got, (d, view, buf, tok, o) = _run(av, z, tokens, T, 0)
+    rng = np.random.default_rng(seed)
+    gl, gh = rng.standard_normal((2, M)).astype(np.float32)
+    g = torch.full_like(view, 9.0)
+    av.aurora_token_logprobs_backward(d, view, tok, o["entropy"], o["lse"], torch.from_numpy(gl).cuda(), torch.from_numpy(gh).cuda(), g)
+    torch.cuda.synchronize()
+    g, zz = g.double().cpu().numpy(), z.double().numpy()
+    half = 2.0 ** -8 if z.dtype == torch.bfloat16 else U
+    hit = np.arange(V)[None] == np.asarray(tokens)[:, None]
+    gl, gh = np.where(hit.any(1), gl, 0.0).astype(np.float64)[:, None], gh.astype(np.float64)[:, None]
+
+    L, H = (got[k].astype(np.float64)[:, None] for k in ("lse", "entropy"))
+    assert np.isfinite(L).all() and np.isfinite(H).all()
+    i = float(np.float32(1.0) / np.float32(T))
+    l = np.clip(zz * i - L, -256.0, 0.0)
+    p, inner = np.exp(l), gl + gh * (l + H)
+    ref = (hit * gl - p * inner) * i
+    off = p * i * (np.abs(inner) * U * (3 * np.abs(l) + 6) + np.abs(gh) * U * np.abs(l) + 4 * U * (np.abs(gl) + np.abs(gh) * (np.abs(l) + H)))
+    off += 2.0 ** -126 * i * np.abs(inner) + 2 * U * i * hit * np.abs(gl)
+    off += half * (np.abs(ref) + off) + 2.0 ** -126
+    assert np.isfinite(g).all() and (np.abs(g - ref) <= off).all(), (np.abs(g - ref) - off).max()
+    if not exact:
+        return
+    x, f = zz / T, token_logprobs(zz, tokens, T)
+    ref = token_logprobs_backward(zz, tokens, T, gl[:, 0], gh[:, 0])
+    lse, H = f["lse"][:, None], f["entropy"][:, None]
+    lp = x - lse
+    p, dist, mean = np.exp(lp), np.abs(x - x.max(1, keepdims=True)), (np.exp(lp) * x).sum(1, keepdims=True)
+    e = U * (2 * dist + 16)
+    pe = (p * e).sum(1, keepdims=True)
+    y = U * (2 * np.abs(x).max(1, keepdims=True) + 2 * np.abs(lse) + np.abs(x) + 16) + pe
+    off_h = 2 * U * (p * (x - mean) ** 2).sum(1, keepdims=True) + (p * e * (np.abs(lp + H) + 1)).sum(1, keepdims=True) + 16 * U * (p * dist).sum(1, keepdims=True) + U * H
+    inner = gl + gh * (lp + H)
+    off = p / T * (np.abs(inner) * (np.expm1(y) + U * (3 * np.abs(lp) + 6)) + np.abs(gh) * np.exp(y) * (y + off_h) + 4 * U * (np.abs(gl) + np.abs(gh) * (np.abs(lp) + H)))
+    off += 2.0 ** -126 / T * np.abs(inner) + 2 * U / T * hit * np.abs(gl)
+    off += half * (np.abs(ref) + off) + 2.0 ** -126
+    assert (np.abs(g - ref) <= off).all(), (np.abs(g - ref) - off).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_rows_with_an_offset(gpu_lib, dtype):
+    """A common offset, or a low temperature, takes digits from p: the logsumexp is handed over in fp32."""
+    rng = np.random.default_rng(51)
+    for bits in (0, 10, 13, 16):
+        for V, T in ((777, 1.0), (5003, 0.7), (5003, 3.0)):
+            z = _logits(60 + bits, 8, V, "f32") + torch.tensor([1.0, -1.0]).repeat(4)[:, None] * (2.0 ** bits if bits else 0.0)
+            _check_gradient(gpu_lib, z.to(DT[dtype]), rng.integers(0, V, 8), T, bits)
+    for T in (0.1, 0.01):
+        _check_gradient(gpu_lib, _logits(61, 8, 5003, dtype), rng.integers(0, 5003, 8), T, 7)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_at_temperatures_far_from_one(gpu_lib, dtype):
+    """Far below one a float32 logsumexp says no more than which entry is the largest, if that: the formula holds with the one given."""
+    for T in (1e-3, 1e-6, 1e-12, 1e-30, 1e-35, 50.0, 1e6):
+        z, tok = _logits(62, 6, 5003, dtype), _tokens(62, 6, 5003)
+        tok[0] = int(z[0].float().argmax())
+        _check_gradient(gpu_lib, z, tok, T, 8, exact=T >= 1.0)
