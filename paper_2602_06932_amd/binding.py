@@ -206,8 +206,26 @@ def _ptrs(*ts):
     return map(_ptr, ts)
 
 
-def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
-    """Device address of a tensor whose rows (dimension 0) may lie apart, as the descriptor's stride says."""
+def _rows_apart(s, n, k: int, stride: int, width: int) -> bool:
+    """Whether the first k dimensions of strides s and sizes n run over rows `stride` elements apart (0: as long as a row), the others over
+    the elements of a row.  width: of a row, where k dimensions are not simply the first one."""
+    dense = 1
+    for i in reversed(range(k, len(n))):
+        if s[i] != dense and n[i] > 1:
+            return False
+        dense *= n[i]
+    if k > 1 and dense < width:
+        return False
+    at = stride or dense
+    for i in reversed(range(k)):
+        if s[i] != at and n[i] > 1:
+            return False
+        at *= n[i]
+    return True
+
+
+def _rows_ptr(t, stride: int, name: str, desc) -> Optional[int]:
+    """Device address of a tensor whose rows may lie apart, as the descriptor's stride says: rows over the first dimension, or the first few."""
     if t is None or t.__class__ is int:
         return t
     if stride == 0 and t.is_contiguous():
@@ -216,13 +234,12 @@ def _rows_ptr(t, stride: int, name: str) -> Optional[int]:
     if stride == n[-1] and t.is_contiguous():  # rows over all dimensions but the last
         return t.data_ptr()
     if stride == 0 or len(s) != 3 or s[0] != stride or s[2] != 1 or s[1] != n[2]:  # (not simply a view of a fused projection's output)
-        dense = 1
-        for k in range(len(n) - 1, 0, -1):
-            if s[k] != dense and n[k] > 1:
-                raise ValueError(f"{name}: the elements of a row must be contiguous")
-            dense *= n[k]
-        if s[0] != (stride or dense) and n[0] > 1:
-            raise ValueError(f"{name}: rows are {s[0]} elements apart, the descriptor says {stride or dense}")
+        if isinstance(desc, aurora_logprob_desc):
+            width = desc.vocab
+        else:
+            width = (desc.num_q_heads if "q" in name else desc.num_kv_heads) * desc.head_dim
+        if not any(_rows_apart(s, n, k, stride, width) for k in range(1, max(2, len(n)))):
+            raise ValueError(f"{name}: no rows of contiguous elements {stride or width} apart, as the descriptor says: sizes {tuple(n)}, strides {s}")
     return t.data_ptr()
 
 
@@ -413,8 +430,8 @@ def aurora_rope_append(desc, q, k, v, positions, slots, frequencies, q_out, k_pa
     """q, k, v and q_out may be tensors whose rows lie apart (views of a fused projection's output): their strides are the descriptor's."""
     lib = load()
     pos, sl, fr, kp, vp = _ptrs(positions, slots, frequencies, k_pages, v_pages)
-    st = lib.aurora_rope_append(_ref(desc), _rows_ptr(q, desc.q_stride, "q"), _rows_ptr(k, desc.k_stride, "k"),
-                                _rows_ptr(v, desc.v_stride, "v"), pos, sl, fr, _rows_ptr(q_out, desc.q_out_stride, "q_out"), kp, vp,
+    st = lib.aurora_rope_append(_ref(desc), _rows_ptr(q, desc.q_stride, "q", desc), _rows_ptr(k, desc.k_stride, "k", desc),
+                                _rows_ptr(v, desc.v_stride, "v", desc), pos, sl, fr, _rows_ptr(q_out, desc.q_out_stride, "q_out", desc), kp, vp,
                                 _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_rope_append")
@@ -423,9 +440,9 @@ def aurora_rope_append(desc, q, k, v, positions, slots, frequencies, q_out, k_pa
 
 def aurora_rope_append_backward(desc, dq_out, dk_pages, dv_pages, positions, slots, frequencies, dq, dk, dv, stream=None,
                                 check=True) -> int:
-    st = load().aurora_rope_append_backward(_ref(desc), _rows_ptr(dq_out, desc.q_out_stride, "dq_out"),
-                                            *_ptrs(dk_pages, dv_pages, positions, slots, frequencies), _rows_ptr(dq, desc.q_stride, "dq"),
-                                            _rows_ptr(dk, desc.k_stride, "dk"), _rows_ptr(dv, desc.v_stride, "dv"), _stream(stream))
+    st = load().aurora_rope_append_backward(_ref(desc), _rows_ptr(dq_out, desc.q_out_stride, "dq_out", desc),
+                                            *_ptrs(dk_pages, dv_pages, positions, slots, frequencies), _rows_ptr(dq, desc.q_stride, "dq", desc),
+                                            _rows_ptr(dk, desc.k_stride, "dk", desc), _rows_ptr(dv, desc.v_stride, "dv", desc), _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_rope_append_backward")
     return st
@@ -451,7 +468,7 @@ def aurora_token_logprobs_workspace_bytes(desc) -> int:
 def aurora_token_logprobs(desc, logits, tokens, logprob, entropy, lse, top_ids, top_logprobs, workspace, stream=None,
                           check=True) -> int:
     """`logits` may be a tensor (its rows may lie apart) or a raw device address (int), e.g. from aurora_verify_logits_ptr()."""
-    st = load().aurora_token_logprobs(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"),
+    st = load().aurora_token_logprobs(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits", desc),
                                       *_ptrs(tokens, logprob, entropy, lse, top_ids, top_logprobs, workspace), workspace.nbytes,
                                       _stream(stream))
     if check and st != AURORA_OK:
@@ -460,9 +477,9 @@ def aurora_token_logprobs(desc, logits, tokens, logprob, entropy, lse, top_ids, 
 
 
 def aurora_token_logprobs_backward(desc, logits, tokens, entropy, lse, dlogprob, dentropy, dlogits, stream=None, check=True) -> int:
-    st = load().aurora_token_logprobs_backward(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits"),
+    st = load().aurora_token_logprobs_backward(_ref(desc), _rows_ptr(logits, desc.row_stride, "logits", desc),
                                                *_ptrs(tokens, entropy, lse, dlogprob, dentropy),
-                                               _rows_ptr(dlogits, desc.row_stride, "dlogits"), _stream(stream))
+                                               _rows_ptr(dlogits, desc.row_stride, "dlogits", desc), _stream(stream))
     if check and st != AURORA_OK:
         raise AuroraError(st, "aurora_token_logprobs_backward")
     return st

@@ -199,3 +199,33 @@ def test_a_change_of_the_alternatives_leaves_the_buffers_of_other_calls(monkeypa
         assert len(a) == len(b) and all(x is y for x, y in zip(a, b))
     first = [x for b in buffers[:3] for x in b]
     assert len({x.data_ptr() for x in first}) == len(first)
+
+
+def test_rows_over_several_dimensions():
+    """Rows that all lie as far apart as the descriptor says are taken in any shape; those that do not are not.  (No rows: the addresses
+    are looked at and nothing is enqueued.)"""
+    wide = torch.zeros(4, 5, 1024)
+    cut, flat = wide[..., :1000], wide.view(20, 1024)[:, :1000]
+    for z in (cut, flat, wide.view(2, 2, 5, 1024)[..., :1000], wide, cut[:1], cut[:, :, :1000]):
+        assert _lp(dict(rows=0, row_stride=1024), logits=z) == av.AURORA_OK
+        assert _lpb(dict(rows=0, row_stride=1024), logits=z, dlogits=z) == av.AURORA_OK
+    for z, why in ((cut[:, :4], "requests of five rows, four of them"), (cut[::2], "every other request"), (cut.transpose(0, 1), "another order"),
+                   (wide[..., ::2], "every other logit"), (wide[..., 0:1000:2], "every other logit"), (cut.unsqueeze(-1).expand(4, 5, 1000, 2), "twice each"),
+                   (torch.zeros(4, 2, 1024)[..., :512], "rows shorter than the vocabulary")):
+        with pytest.raises(ValueError):
+            _lp(dict(rows=0, row_stride=1024), logits=z)
+        with pytest.raises(ValueError):
+            _lpb(dict(rows=0, row_stride=1024), logits=z)
+    with pytest.raises(ValueError):
+        _lp(dict(rows=0), logits=cut)                       # the descriptor says: side by side
+    qkv = torch.zeros(3, 5, 12 * 64, dtype=torch.bfloat16)  # a projection's output for requests of five tokens
+    q, k, v = (x.unflatten(-1, (-1, 64)) for x in qkv.split([512, 128, 128], -1))
+    d = dict(rows=0, q_stride=768, k_stride=768, v_stride=768)
+    for back in (False, True):
+        assert _rope(d, back=back, q=q, k=k, v=v) == av.AURORA_OK
+        assert _rope(d, back=back, q=q.flatten(0, 1), k=k.flatten(0, 1), v=v.flatten(0, 1)) == av.AURORA_OK
+        for bad in (q[:, :4], q[:, :, ::2], q[..., ::2], q.transpose(1, 2)):
+            with pytest.raises(ValueError):
+                _rope(d, back=back, q=bad, k=k, v=v)
+        with pytest.raises(ValueError):                     # heads as far apart as rows should be
+            _rope(d, back=back, q=torch.zeros(3, 8, 768, dtype=torch.bfloat16)[..., :64], k=k, v=v)
