@@ -542,7 +542,8 @@ int aurora_cache_plan(const aurora_cache_plan_desc* desc, const int32_t* held_le
  * magnitude included, the turn transposed.  An 8-bit cache is refused (AURORA_ERR_UNSUPPORTED).
  *
  * Pointers need the alignment of their element type; whole 16-byte vectors are used where all arrays, strides and rotary_dim allow.
- * No workspace.  AURORA_ERR_UNSUPPORTED for more than 2^22 rows, head_dim > 256, more than 2^31 - 1 slots.
+ * No workspace.  AURORA_ERR_UNSUPPORTED for more than 2^22 rows, 65535 heads or 2^31 - 1 slots, head_dim > 256, or more rows times heads than one
+ * launch takes (some 5 x 10^11 elements).
  */
 typedef struct {
   int32_t rows;              /* T >= 0 (0: nothing is enqueued)                               */

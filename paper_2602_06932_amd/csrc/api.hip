@@ -625,6 +625,20 @@ int check_cache_plan(const aurora_cache_plan_desc* d) {
   return AURORA_OK;
 }
 
+RopeLaunch rope_launch_from(const aurora_rope_desc* d) {
+  RopeLaunch a = {};
+  a.rows = d->rows; a.Hq = d->num_q_heads; a.Hkv = d->num_kv_heads; a.D = d->head_dim; a.rotary = d->rotary_dim;
+  a.page = d->num_kv_heads > 0 ? d->page_size : 1;
+  a.num_slots = d->num_kv_heads > 0 ? (int)(d->num_pages * d->page_size) : 0;
+  a.interleaved = d->interleaved != 0; a.bf16 = d->dtype == AURORA_BF16; a.kv_fp8 = d->kv_fp8 != 0 && d->num_kv_heads > 0;
+  a.k_scale = d->k_scale; a.v_scale = d->v_scale;
+  a.magnitude = d->magnitude > 0.f ? d->magnitude : 1.f;
+  const int64_t q = (int64_t)d->num_q_heads * d->head_dim, kv = (int64_t)d->num_kv_heads * d->head_dim;
+  a.q_stride = d->q_stride ? d->q_stride : q; a.q_out_stride = d->q_out_stride ? d->q_out_stride : q;
+  a.k_stride = d->k_stride ? d->k_stride : kv; a.v_stride = d->v_stride ? d->v_stride : kv;
+  return a;
+}
+
 int check_rope(const aurora_rope_desc* d) {
   if (!d || d->rows < 0 || d->num_q_heads < 0 || d->num_kv_heads < 0 || d->num_q_heads + (int64_t)d->num_kv_heads < 1 ||
       d->head_dim < 1 || d->rotary_dim < 0 || d->rotary_dim > d->head_dim || d->rotary_dim % 2)
@@ -645,21 +659,7 @@ int check_rope(const aurora_rope_desc* d) {
     return AURORA_ERR_INVALID_ARG;
   if (d->head_dim > kRopeMaxDim || d->rows > kRopeMaxRows || d->num_q_heads > 65535 || d->num_kv_heads > 65535)
     return AURORA_ERR_UNSUPPORTED;
-  return AURORA_OK;
-}
-
-RopeLaunch rope_launch_from(const aurora_rope_desc* d) {
-  RopeLaunch a = {};
-  a.rows = d->rows; a.Hq = d->num_q_heads; a.Hkv = d->num_kv_heads; a.D = d->head_dim; a.rotary = d->rotary_dim;
-  a.page = d->num_kv_heads > 0 ? d->page_size : 1;
-  a.num_slots = d->num_kv_heads > 0 ? (int)(d->num_pages * d->page_size) : 0;
-  a.interleaved = d->interleaved != 0; a.bf16 = d->dtype == AURORA_BF16; a.kv_fp8 = d->kv_fp8 != 0 && d->num_kv_heads > 0;
-  a.k_scale = d->k_scale; a.v_scale = d->v_scale;
-  a.magnitude = d->magnitude > 0.f ? d->magnitude : 1.f;
-  const int64_t q = (int64_t)d->num_q_heads * d->head_dim, kv = (int64_t)d->num_kv_heads * d->head_dim;
-  a.q_stride = d->q_stride ? d->q_stride : q; a.q_out_stride = d->q_out_stride ? d->q_out_stride : q;
-  a.k_stride = d->k_stride ? d->k_stride : kv; a.v_stride = d->v_stride ? d->v_stride : kv;
-  return a;
+  return rope_fits(rope_launch_from(d)) ? AURORA_OK : AURORA_ERR_UNSUPPORTED;
 }
 
 // the arrays that both directions have; rows and the other side's are typed by the caller

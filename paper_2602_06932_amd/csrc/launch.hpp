@@ -186,7 +186,8 @@ struct RopeLaunch {
   void *q_out, *k_pages, *v_pages;
   int block_rows, chunks, page_shift;                                  // set by the launcher
 };
-constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;   // so that a block's angles fit into LDS
+constexpr int kRopeMaxRows = 1 << 22, kRopeMaxDim = 256;
+bool rope_fits(const RopeLaunch& P);                       // a block's angles into LDS
 hipError_t launch_rope(const RopeLaunch& P, bool back, hipStream_t st);
 
 // log probabilities of given tokens, entropy, alternatives, and the gradient (see logprob.hip)

@@ -269,20 +269,31 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeLaunch P) {
   }
 }
 
+// workgroups that a row is cut into where a vector has n elements
+static int rope_chunks(const RopeLaunch& P, int n) {
+  const int units = (P.Hq + P.Hkv) * (P.rotary / 2 / n + (P.D - P.rotary + 2 * n - 1) / (2 * n)) + P.Hkv * ((P.D + 2 * n - 1) / (2 * n));
+  return (units + kRopeThreads - 1) / kRopeThreads;
+}
+// One row a block while the launch would not fill the chip, then as many as are loaded ahead: more only make a block's start longer
+// (two a block, four, eight, sixteen: 16384 rows of 32 + 8 + 8 heads of 128 77, 77, 82, 99 us, their gradients 54.5, 58.5, 63, 63).
+static int64_t rope_block_rows(const RopeLaunch& P, int chunks) {
+  int64_t rows = (int64_t)chunks * P.rows / kRopeAhead >= 2048 ? kRopeAhead : 1;
+  while ((P.rows + rows - 1) / rows * chunks > ((int64_t)1 << 32) / kRopeThreads - 1) rows *= 2;  // fewer than 2^32 threads
+  return rows;
+}
+static size_t rope_lds(const RopeLaunch& P, int64_t block_rows) { return (size_t)block_rows * (P.rotary / 2) * sizeof(f32x2_t); }
+
+// (single elements are the most workgroups a row, and so the most rows a block)
+bool rope_fits(const RopeLaunch& P) { return rope_lds(P, rope_block_rows(P, rope_chunks(P, 1))) <= 64 * 1024; }
+
 template <typename T, typename TC, bool kPairs, int kN, bool kBack>
 static hipError_t launch_rope_k(RopeLaunch P, hipStream_t st) {
-  const int half = P.rotary / 2;
-  const int units = (P.Hq + P.Hkv) * (half / kN + (P.D - P.rotary + 2 * kN - 1) / (2 * kN)) + P.Hkv * ((P.D + 2 * kN - 1) / (2 * kN));
   P.page_shift = (P.page & (P.page - 1)) == 0 ? __builtin_ctz(P.page) : -1;
-  P.chunks = (units + kRopeThreads - 1) / kRopeThreads;
-  // One row a block while the launch would not fill the chip, then as many as are loaded ahead: more only make a block's start longer
-  // (two a block, four, eight, sixteen: 16384 rows of 32 + 8 + 8 heads of 128 77, 77, 82, 99 us, their gradients 54.5, 58.5, 63, 63).
-  int64_t rows = (int64_t)P.chunks * P.rows / kRopeAhead >= 2048 ? kRopeAhead : 1;
-  while ((P.rows + rows - 1) / rows * P.chunks > ((int64_t)1 << 32) / kRopeThreads - 1) rows *= 2;  // fewer than 2^32 threads
+  P.chunks = rope_chunks(P, kN);
+  const int64_t rows = rope_block_rows(P, P.chunks);
   P.block_rows = (int)rows;
-  const size_t lds = (size_t)rows * half * sizeof(f32x2_t);
-  if (lds > 64 * 1024) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((rope_kernel<T, TC, kPairs, kN, kBack>), dim3((unsigned)((P.rows + rows - 1) / rows * P.chunks)), dim3(kRopeThreads), lds, st, P);
+  hipLaunchKernelGGL((rope_kernel<T, TC, kPairs, kN, kBack>), dim3((unsigned)((P.rows + rows - 1) / rows * P.chunks)), dim3(kRopeThreads),
+                     rope_lds(P, rows), st, P);
   return hipGetLastError();
 }
 

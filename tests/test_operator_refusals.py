@@ -229,3 +229,11 @@ def test_rows_over_several_dimensions():
                 _rope(d, back=back, q=bad, k=k, v=v)
         with pytest.raises(ValueError):                     # heads as far apart as rows should be
             _rope(d, back=back, q=torch.zeros(3, 8, 768, dtype=torch.bfloat16)[..., :64], k=k, v=v)
+
+
+def test_rope_rows_too_wide_for_so_many():
+    """A launch has less than 2^32 threads: past that a block takes more rows, and their angles have to fit into its LDS."""
+    for back in (False, True):
+        for rotary in (2, 64, 256):
+            assert _rope(dict(rows=2 ** 22, num_q_heads=65535, num_kv_heads=65535, head_dim=256, rotary_dim=rotary), back=back) == NOT
+        assert _rope(dict(rows=2 ** 22, num_q_heads=65535, num_kv_heads=1, head_dim=256, rotary_dim=256), back=back) == NOT
