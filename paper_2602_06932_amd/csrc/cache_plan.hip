@@ -12,11 +12,12 @@
 // entries that are read lie below those that are written.  Tokens of a page taken in this call find it the same way, not through
 // the table.
 //
-// Bound by latency: a launch, the lengths, a search and one or two loads in turn - 4.0 us for 32 requests of five tokens, 5.6 for 256
-// that grow, shrink, end and begin with 112 000 rows, 7.4 for a million rows, of which writing their positions and slots is 1.6 at a
-// copy's rate.  Up to 1024 requests every workgroup forms the prefix sums itself, four requests a thread, and does its share of the
-// writing: one launch.  Where more than one workgroup is wanted and an output is the input that the others still read, or there are
-// more requests, one workgroup plans into the workspace and a second launch writes.
+// Bound by latency: a launch, the lengths, a search and one or two loads in turn - 4.2 us a call in a captured graph for 32 requests of
+// five tokens, 5.1 for 256 that grow, shrink, end and begin with 120 000 rows, 7.0 for a million rows, of which writing their positions and
+// slots is 1.6 at a copy's rate.  Up to 1024 requests every workgroup forms the prefix sums itself, four requests a thread, and does its
+// share of the writing: one launch.  Where more than one workgroup is wanted and an output is the input that the others still read, or there
+// are more requests, one workgroup plans into the workspace and a second launch writes: the same three in place 6.6, 8.6 and 10.2 us, 2000
+// requests of five tokens 15.4.
 #include "launch.hpp"
 
 #include <algorithm>
@@ -296,9 +297,10 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_requests_kernel(Cache
   const PlanTotals t = plan_requests<false>(P, workspace_arrays(P), true);
   if (threadIdx.x == 0) *(int4*)P.work = make_int4(t.n, t.freed, t.taken, t.rows);
 }
+template <int kRows>
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_write_kernel(CachePlanLaunch P) {
   const int4 t = *(const int4*)P.work;
-  plan_write<4>(P, workspace_arrays(P), PlanTotals{t.x, t.y, t.z, t.w});
+  plan_write<kRows>(P, workspace_arrays(P), PlanTotals{t.x, t.y, t.z, t.w});
 }
 
 size_t cache_plan_work_bytes(int batch) { return 16 + 5 * ((size_t)batch + 1) * sizeof(int32_t); }
@@ -307,8 +309,9 @@ hipError_t launch_cache_plan(const CachePlanLaunch& plan, hipStream_t st) {
   CachePlanLaunch P = plan;
   P.page_shift = (P.page & (P.page - 1)) == 0 ? __builtin_ctz(P.page) : -1;
   // Few rows are given a thread each: four that belong to two or three requests are as many loads in turn (us with one and with four:
-  // 160 rows 4.0 and 6.1, 112 000 5.6 and 9.0, 2^20 9.7 and 7.5, where writes of 16 bytes count).  A workgroup per 256 or 1024
-  // rows, and per 4096 cells of the table (how many cells change hands only the lengths say).
+  // 160 rows 4.0 and 6.1, 120 000 5.6 and 9.0, 2^20 9.7 and 7.5, where writes of 16 bytes count; in the second of two launches 160 6.6
+  // and 9.0, 120 000 8.6 and 13.0).  A workgroup per 256 or 1024 rows, and per 4096 cells of the table (how many cells change hands
+  // only the lengths say).
   const bool few = P.max_rows <= kPlanFewRows;
   const int64_t rows = P.slots ? ((int64_t)P.max_rows + (few ? 255 : 1023)) / (few ? 256 : 1024) : 0;
   const int64_t cells = (int64_t)P.B * P.max_pages / 4096;
@@ -322,7 +325,8 @@ hipError_t launch_cache_plan(const CachePlanLaunch& plan, hipStream_t st) {
   }
   hipLaunchKernelGGL(cache_plan_requests_kernel, dim3(1), dim3(kPlanThreads), 0, st, P);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL(cache_plan_write_kernel, dim3(grid), dim3(kPlanThreads), 0, st, P);
+  if (few) hipLaunchKernelGGL(cache_plan_write_kernel<1>, dim3(grid), dim3(kPlanThreads), 0, st, P);
+  else hipLaunchKernelGGL(cache_plan_write_kernel<4>, dim3(grid), dim3(kPlanThreads), 0, st, P);
   return hipGetLastError();
 }
 

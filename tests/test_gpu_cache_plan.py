@@ -177,3 +177,13 @@ def test_a_call_may_be_repeated_and_captured(gpu_lib):
         for a, b in zip(o, ("count", "seq_lens", "row_start", "positions", "slots", "info")):
             assert np.array_equal(a.cpu().numpy(), np.atleast_1d(ref[b])), b
         assert np.array_equal(t.cpu().numpy(), ref["table"]) and np.array_equal(f.cpu().numpy(), ref["free"])
+
+
+@pytest.mark.parametrize("batch,width,page", [(40, 450, 16), (1100, 20, 16), (1030, 13, 24)])
+@pytest.mark.parametrize("spare", [0, 1, 1030])
+def test_plans_of_two_launches_on_both_sides_of_a_row_a_thread(gpu_lib, batch, width, page, spare):
+    """In place over many workgroups, and more requests than one plans at a time: up to 2^18 rows, and just past them."""
+    rng = np.random.default_rng(batch + spare)
+    s = _state(rng, batch, page, width, grow=0.6)
+    _check(gpu_lib, *s, page, 2 ** 18 + spare, in_place=True)
+    _check(gpu_lib, *s, page, 2 ** 18 + spare, shift=spare % 2)
