@@ -484,8 +484,8 @@ int aurora_draft_loss(const aurora_loss_desc* desc, const float* draft_logits, c
  * and its slot (page * page_size + offset) in the pools.
  *
  * Request b holds held_lens[b] tokens (NULL: none does) and is to hold want_lens[b]:
- *   fewer   its pages past ceil(want / page_size) go back on top of the stack of free pages (drafts that were rejected, and with 0
- *           a request that has ended)
+ *   fewer   its pages past ceil(want / page_size) go back on top of the stack of free pages (drafts of a chain that were rejected, and
+ *           with 0 a request that has ended)
  *   more    pages are taken from the top of the stack for it
  * All pages given back (requests in order, pages in order) are pushed before the first is taken (in the same order).
  * A request that wants more is refused, and keeps what it holds, if the stack runs out at it, or the rows do (max_rows); every later
@@ -500,6 +500,10 @@ int aurora_draft_loss(const aurora_loss_desc* desc, const float* draft_logits, c
  *   positions, slots [max_rows]         of every row; from row_start[B] on 0 and -1.  Not used if max_rows is 0: nothing is
  *                                       then refused for want of rows.
  *   info        [4] or NULL             rows, pages taken, pages given back, requests refused
+ * A request's tokens lie in the order of their positions, and what it keeps is a prefix of them: prompts and chains.  The nodes of a draft
+ * tree get pages and slots as well (node n's at seq_len - num_q + n, where the attention looks for it), but positions[] counts the
+ * nodes - siblings share a position, which the caller has to write - and an accepted path is in general no prefix of the nodes: a shorter
+ * length keeps the first nodes, not the path.  Its keys and values have to be brought to the front before the others' pages go back.
  * The result is unique, hence bit-reproducible.  Given distinct free_count_out and seq_lens the call may be repeated on the
  * same state with the same result.  Up to 1024 requests and distinct outputs it is one launch, otherwise up to two.
  * AURORA_ERR_UNSUPPORTED for more than 2^31 - 1 slots or table cells, or rows of the table longer than 2^30 tokens.

@@ -1,5 +1,5 @@
 // Block tables and slot maps of the paged KV cache, built on the GPU from request lengths.  After a verification step (paper
-// section 2.1: a prefix of the drafts is kept) only the GPU knows how long each request has become; this plans the pages of
+// section 2.1: a prefix of a chain's drafts is kept) only the GPU knows how long each request has become; this plans the pages of
 // the next one without a trip to the host.
 //
 //   pages(n) = ceil(n / page).  A request that holds h tokens and is to hold w gives pages(h) - pages(w) back if w < h, and takes
