@@ -498,3 +498,36 @@ def test_gradients_at_temperatures_far_from_one(gpu_lib, dtype):
         z, tok = _logits(62, 6, 5003, dtype), _tokens(62, 6, 5003)
         tok[0] = int(z[0].float().argmax())
         _check_gradient(gpu_lib, z, tok, T, 8, exact=T >= 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_of_requests_cut_from_a_padded_vocabulary(gpu_lib, dtype):
+    """[B, Nq, V] out of [B, Nq, Vpad], forward and gradient: what the rows side by side give, and nothing in the padding."""
+    av = gpu_lib
+    B, Nq, V, Vpad = 3, 5, 3001, 3008
+    code = av.AURORA_F32 if dtype == "f32" else av.AURORA_BF16
+    wide = torch.full((B, Nq, Vpad), 100.0, dtype=DT[dtype], device="cuda")
+    cut = wide[..., :V]
+    cut.copy_(_logits(63, B * Nq, V, dtype).view(B, Nq, V))
+    tok = torch.from_numpy(np.random.default_rng(63).integers(0, V, (B, Nq)).astype(np.int32)).cuda()
+    got = []
+    for z, stride in ((cut, Vpad), (cut.contiguous(), 0)):
+        d = av.aurora_logprob_desc(rows=B * Nq, vocab=V, dtype=code, n_top=3, row_stride=stride)
+        ws = torch.empty(av.aurora_token_logprobs_workspace_bytes(d), dtype=torch.uint8, device="cuda")
+        lp, H, lse = (torch.zeros(B, Nq, device="cuda") for _ in range(3))
+        ti, tl = torch.zeros((B, Nq, 3), dtype=torch.int32, device="cuda"), torch.zeros((B, Nq, 3), device="cuda")
+        g = torch.full_like(wide, 9.0)[..., :V] if stride else torch.zeros_like(z)
+        av.aurora_token_logprobs(d, z, tok, lp, H, lse, ti, tl, ws)
+        av.aurora_token_logprobs_backward(d, z, tok, H, lse, lp, H, g)
+        torch.cuda.synchronize()
+        if stride:
+            assert bool((g._base[..., V:] == 9.0).all()) and bool((wide[..., V:] == 100.0).all())
+        got.append((lp, H, lse, ti, tl, g))
+    assert torch.equal(got[0][3], got[1][3])
+    # rows that start elsewhere within 16 bytes are summed in another order.  |x| below 13, distances below 25: by the bounds above each
+    # result is off by less than 2u 13 + u (2 25 + 16) + u 13 = 105 u, the entropy by less than ten times that; gradients of log
+    # probabilities and entropies below 25 by less than 25 times that, and by a step of their type where they round apart
+    for a, b in zip(got[0][:3] + got[0][4:5], got[1][:3] + got[1][4:5]):
+        assert (a - b).abs().max() <= 2 * 1050 * U
+    a, b = (x[5].double() for x in got)
+    assert ((a - b).abs() <= 2 * 2625 * U + 2 * (2.0 ** -8 if dtype == "bf16" else U) * torch.maximum(a.abs(), b.abs()) * (1 + 2.0 ** -7)).all()

@@ -294,3 +294,33 @@ def test_log_probabilities_of_requests_with_their_own_temperatures(gpu_lib):
         assert np.allclose(dv.logprob.cpu().numpy().reshape(-1), ref["logprob"], rtol=1e-6, atol=8e-6)
         assert np.allclose(dv.lse.cpu().numpy().reshape(-1), ref["lse"], rtol=1e-6, atol=8e-6)
         assert np.array_equal(dv.top_ids.cpu().numpy(), ref["top_ids"])
+
+
+def test_captured_log_probabilities_beside_calls_with_other_alternatives(gpu_lib):
+    """A graph goes on giving its own results after calls with other numbers of alternatives, and leaves theirs alone."""
+    from paper_2602_06932_amd.device import DeviceVerify
+    w = gen.llama_chain(4, batch=3, len_lo=40, len_hi=300, vocab=70001, hidden_size=512)
+    dv = DeviceVerify(w)
+    dv.verify()
+    tokens = dv.next_token[:, None].expand(-1, w.num_q).contiguous()
+    dv.logprobs(tokens, n_top=5)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        dv.logprobs(tokens, n_top=5)
+    mine = [dv.logprob, dv.entropy, dv.lse, dv.top_ids, dv.top_logprobs]
+    ref = token_logprobs(dv.logits_host().reshape(-1, w.vocab).astype(np.float64), tokens.cpu().numpy().reshape(-1), w.temperature, 5)
+    for n_top in (0, 32, 5):
+        dv.logprobs(tokens, n_top=n_top)
+        others = [x for x in (dv.logprob, dv.entropy, dv.lse, dv.top_ids, dv.top_logprobs) if x is not None]
+        if n_top != 5:
+            for x in others:
+                x.fill_(-3)
+        for x in mine:
+            x.fill_(-9)
+        junk = [torch.full((1 << k,), 7, dtype=torch.uint8, device="cuda") for k in range(4, 18)]
+        g.replay()
+        torch.cuda.synchronize()
+        assert np.allclose(mine[0].cpu().numpy().reshape(-1), ref["logprob"], atol=8e-6) and np.array_equal(mine[3].cpu().numpy(), ref["top_ids"])
+        assert np.allclose(mine[1].cpu().numpy().reshape(-1), ref["entropy"], atol=2e-5) and np.allclose(mine[4].cpu().numpy(), ref["top_logprobs"], atol=8e-6)
+        assert all(bool((x == 7).all()) for x in junk) and (n_top == 5 or all(bool((x == -3).all()) for x in others))
