@@ -526,10 +526,10 @@ def test_logits_of_requests_cut_from_a_padded_vocabulary(gpu_lib, dtype):
     assert torch.equal(got[0][3], got[1][3])
     # Rows that start elsewhere within 16 bytes are summed in another order.  |x| below 13, distances below 25: by the bounds above each
     # result is off by less than 2u 13 + u (2 25 + 16) + u 13 = 105 u, the entropy (below 8.1) by less than ten times that, p by 118 u.  No
-    # p above a half: the gradient is off by 105 u + 25 p 118 u, by 8.1 p (10 118 + 1050 + 118) u and by 1050 p 10 u, 17 000 u together, and
+    # p above 0.6: the gradient is off by 105 u + 25 p 118 u, by 8.1 p (10 118 + 1050 + 118) u and by 1050 p 10 u, 20 000 u together, and
     # by half a step of its type
     for a, b in zip(got[0][:3] + got[0][4:5], got[1][:3] + got[1][4:5]):
         assert (a - b).abs().max() <= 2 * 1050 * U
-    assert got[0][4].max() < -0.7
+    assert got[0][4].max() < np.log(0.6)
     a, b = (x[5].double() for x in got)
-    assert ((a - b).abs() <= 2 * 17000 * U + 2 * (2.0 ** -8 if dtype == "bf16" else U) * torch.maximum(a.abs(), b.abs())).all()
+    assert ((a - b).abs() <= 2 * 20000 * U + 2 * (2.0 ** -8 if dtype == "bf16" else U) * torch.maximum(a.abs(), b.abs())).all()
