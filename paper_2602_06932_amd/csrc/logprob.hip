@@ -19,9 +19,15 @@
 // values in the order of their ids.
 //
 // The logits are read with loads that do not stay in the caches, unless a gradient is likely to follow (kLpKeepBytes): 4096 x 32000 fp32
-// 126 -> 80 us = 6.5 TB/s, what a read of memory gives; 1280 x 200064 bf16 with eight alternatives 87 us = 5.9; 160 x 128256 fp32 with twenty 21 and 4 for the merge: from 128 to
-// 320 rows 0.085 us a row = 6.0 TB/s, and 10 us of launches, first loads, selection and merge.  The gradient: 4096 x 32000 fp32 201 us
-// (171 after a forward that left logits in the caches), 1024 x 128256 bf16 100 = 5.2 TB/s, as a device copy.
+// 126 -> 80 us = 6.5 TB/s, what a read of memory gives; 1280 x 200064 bf16 with eight alternatives 87 us = 5.9.  The gradient: 4096 x 32000
+// fp32 201 us (171 after a forward that left logits in the caches), 1024 x 128256 bf16 100 = 5.2 TB/s, as a device copy.
+//
+// Rows cut into parts with alternatives are further from it: 160 x 128256 fp32 with twenty 21 us and 4 for the merge, where the read takes
+// 12.4; 160 x 151936 bf16 26 in all, where it takes 7.4.  A part is loaded whole, then summed, then searched: 20 vector instructions an
+// element, to the streaming kernel's 10 (fp32, without alternatives) or 8 (bf16, with), and after the read rather than under it.  Nor do all
+// parts start together: 113 registers hold 1024 workgroups of the first call's 1280, 138 hold 768 of the second's 800.  Short rows are a chain each -
+// load, two 64-bit sums, a logarithm - in a wavefront that has nothing of its next row on the way (60000 x 777 fp32 49 us, the read 28); with
+// alternatives the blocks that hold one are read from memory again, and listed in LDS (96).
 #include "launch.hpp"
 
 #include <float.h>

@@ -14,7 +14,9 @@
 // sine and cosine of what is left in 32.
 //
 // 16384 rows of 32 + 8 + 8 heads of 128, bf16: 77 us = 5.2 TB/s, what a device copy of as many bytes takes; the gradients of 8192 57 us
-// = 5.3; 8192 rows of 48 + 8 + 8 into an 8-bit cache, half of each head turned, 52 us = 4.8; 160 rows 3.8 us.
+// = 5.3; 8192 rows of 48 + 8 + 8 into an 8-bit cache, half of each head turned, 52 us = 4.8; 160 rows 3.8 us; 8192 rows in fp32 80 us =
+// 5.0, their gradients 79.  Where 16-byte vectors do not fit, an element an access: 8192 rows of 32 + 8 + 8 an element further apart 101 us
+// for 42, their gradients 97 for 56; of 9 + 3 + 3 heads of 80 with 40 turned 25 us, with all 80 12, their gradients 23.5 and 13.4.
 #include "launch.hpp"
 
 #include <algorithm>
@@ -65,9 +67,11 @@ __device__ __forceinline__ unsigned e4m3_pack4(float a, float b, float c, float 
   return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(c), e4m3_range(d), w, true);
 }
 
-// The one rounding of a result: to the type it is kept in.  kPast: past the caches, for rows, not for the pools, which the attention reads
-// next, nor beside an 8-bit cache (32768 rows of 48 + 8 + 8 heads 182 us, 186 past them): 4096 rows of 32 + 8 + 8 23.4 -> 19.7, their
-// gradients 31.6 -> 28.3, 16384 rows 78.4 -> 77.2.  (Loads past them: gradients of 8192 57 -> 66.)
+// The one rounding of a result: to the type it is kept in.  kPast: past the caches, for rows, not for the pools, nor beside an 8-bit cache
+// (32768 rows of 48 + 8 + 8 heads 182 us, 186 past them): 4096 rows of 32 + 8 + 8 23.4 -> 19.7, their gradients 31.6 -> 28.3, 16384 rows
+// 78.4 -> 77.2.  The attention, which reads the turned queries next, does not lose by it: the two calls in turn, past the caches and not, 160
+// rows 26.5 and 26.8 us (contexts of 512), 55.5 and 55.7 (2048), 1280 rows 215.6 and 215.9, 4096 277.5 and 277.6.  (Loads past them:
+// gradients of 8192 57 -> 66.)
 template <int N, bool kPast = false, typename T>
 __device__ __forceinline__ void store_vec(T* p, const float (&x)[N]) {
   auto put = [](auto w, auto* at) {
